@@ -349,6 +349,127 @@ ember_status ember_set_trace_events(ember_handle *h, void *const *events, int n)
  * the failure path is tested.  Host only. */
 ember_status ember_set_wait_limit_ns(ember_handle *h, uint64_t ns);
 
+/* ---------------------------------------------------------------------------
+ * Operators around the step: what makes a head's hidden states and dlogits,
+ * what is done to gradients before a step, and the 8-bit head that serves
+ * the trained table.  They need no handle.  Matrices are row-major with a
+ * row stride (ld..., in elements, at least the row length) and need the
+ * alignment of their elements only; rows that start on 16 bytes take wider
+ * accesses.  Scratch ("workspace", 16-byte aligned, contents irrelevant
+ * before and after) belongs to the caller, as does the sticky status word
+ * that some of them set where only the GPU can see an error.  Sums,
+ * statistics and products are held in 32 bits or more and each output is
+ * rounded once.  Results are the same bits on every run.
+ * ------------------------------------------------------------------------- */
+
+/* A sticky status word: one unsigned in device memory.  init zeroes it on
+ * `stream`; read synchronises the stream, returns EMBER_OK,
+ * EMBER_ERR_ID_OUT_OF_RANGE or EMBER_ERR_TIMEOUT and clears it. */
+ember_status ember_status_init(unsigned *status, void *stream);
+ember_status ember_status_read(unsigned *status, void *stream);
+
+/* Residual addition and root-mean-square norm of T rows of D values:
+ *   s = x + residual,  h = s,  y_j = gain_j s_j / sqrt(mean_j s_j^2 + eps).
+ *   x:        T x D of xtype; y (T x D, xtype) is written and may be x.
+ *   residual: T x D of rtype, or NULL (then h is NULL too and s = x);
+ *   h:        the sum rounded to rtype, for the next layer and the backward
+ *             pass; may be residual.  y is formed from the sum before that
+ *             rounding.
+ *   gain:     D values of gtype, or NULL for ones.
+ *   eps >= 0, finite.  D <= 32768 (EMBER_ERR_UNSUPPORTED).  T = 0 does
+ * nothing.  The squares are summed in fp32: values beyond about 1e19 give
+ * an infinite mean and y = 0. */
+ember_status ember_rmsnorm(const void *x, int64_t ldx, ember_wdtype xtype,
+                           const void *residual, int64_t ldr, ember_wdtype rtype,
+                           const void *gain, ember_wdtype gtype, int64_t T, int64_t D, float eps,
+                           void *h, int64_t ldh, void *y, int64_t ldy, void *stream);
+
+/* The same with y in 8 bits: scales[t] = max_j |y_tj| / 127 and
+ * q_tj = y_tj / scales[t] rounded to nearest even, |q| <= 127, so that
+ * y_tj is about q_tj scales[t].  A row of zeros has the scale 0; a row with
+ * an infinity or a NaN has the scale NaN and zeros in q. */
+ember_status ember_rmsnorm_quant(const void *x, int64_t ldx, ember_wdtype xtype,
+                                 const void *residual, int64_t ldr, ember_wdtype rtype,
+                                 const void *gain, ember_wdtype gtype, int64_t T, int64_t D, float eps,
+                                 void *h, int64_t ldh, int8_t *q, int64_t ldq, float *scales, void *stream);
+
+/* 8-bit rows of any T x D matrix (a trained table, once per table), with the
+ * scales and the rounding of ember_rmsnorm_quant, and back: y = q scale. */
+ember_status ember_quantize_rows(const void *x, int64_t ldx, ember_wdtype xtype, int64_t T, int64_t D,
+                                 int8_t *q, int64_t ldq, float *scales, void *stream);
+ember_status ember_dequantize_rows(const int8_t *q, int64_t ldq, const float *scales, int64_t T, int64_t D,
+                                   void *y, int64_t ldy, ember_wdtype ytype, void *stream);
+
+/* Gradients of the norm at h (the sum that ember_rmsnorm stored), with
+ * n_t = sqrt(mean_j h_tj^2 + eps):
+ *   dx_tj = gain_j dy_tj / n_t - h_tj (sum_k gain_k dy_tk h_tk) / (D n_t^3) + dres_tj
+ *   dgain_j = sum_t dy_tj h_tj / n_t       (fp32, D values, written)
+ * dx is the gradient of x and of residual alike; dres (or NULL) is what
+ * reaches h past the norm.  dy, h, dres and dx are T x D of `type`; dx may
+ * be dy or dres.  T = 0 writes a zero dgain.  workspace:
+ * ember_rmsnorm_backward_workspace_bytes(T, D) (0 for sizes that are
+ * refused). */
+size_t ember_rmsnorm_backward_workspace_bytes(int64_t T, int64_t D);
+ember_status ember_rmsnorm_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh,
+                                    const void *dres, int64_t lddres, ember_wdtype type,
+                                    const void *gain, ember_wdtype gtype, int64_t T, int64_t D, float eps,
+                                    void *dx, int64_t lddx, float *dgain,
+                                    void *workspace, size_t bytes, void *stream);
+
+/* Product of 8-bit integers with a scale per token and per channel:
+ *   out[t][v] = xs[t] ws[v] sum_k xq[t][k] wq[v][k]
+ *   xq: T x K int8 with xs (T), wq: V x K int8 with ws (V); any values in
+ *   [-128, 127].  out: T x V of otype, written.  K <= 32768.
+ * T = 0 does nothing.  workspace: ember_matmul_quant_workspace_bytes(T, V,
+ * K).  status (not NULL): EMBER_ERR_TIMEOUT if a bounded wait gave up. */
+size_t ember_matmul_quant_workspace_bytes(int64_t T, int64_t V, int64_t K);
+ember_status ember_matmul_quant(const int8_t *xq, int64_t ldx, const float *xs,
+                                const int8_t *wq, int64_t ldw, const float *ws,
+                                int64_t T, int64_t V, int64_t K, void *out, int64_t ldo, ember_wdtype otype,
+                                void *workspace, size_t bytes, unsigned *status, void *stream);
+
+/* Softmax cross-entropy of T tokens over V entries, with the gradient of the
+ * logits (the dlogits that ember_step_lmhead takes):
+ *   nll_t = log sum_v exp(z_tv) - z_t,y_t,  0 for a token that does not count
+ *   g_t = w_t / n with mean = 1 (n tokens count), w_t with mean = 0
+ *   loss = sum_t g_t nll_t,  dz_tv = g_t (softmax(z_t)_v - [v = y_t])
+ *   logits:  T x V of ztype; -inf masks an entry out.
+ *   targets: T ids of idtype.  A token whose target is ignore_index does not
+ *            count; one whose target is otherwise outside [0, V) does not
+ *            either, and sets EMBER_ERR_ID_OUT_OF_RANGE in *status.
+ *   weights: T fp32 (advantages of a policy gradient, say), or NULL for 1.
+ *   loss: one fp32; nll: T fp32; both written.
+ *   dlogits: T x V of dtype, written, or NULL when no gradient is wanted;
+ *            may be logits (same type and stride).  Rows of tokens that do
+ *            not count are zero.
+ * A row that is -inf throughout has no distribution: its nll is +inf and its
+ * gradient zero.  A NaN or +inf among a row's logits makes the row's nll and
+ * gradient NaN.  With no token counted the loss is 0.  workspace:
+ * ember_softmax_loss_workspace_bytes(T). */
+size_t ember_softmax_loss_workspace_bytes(int64_t T);
+ember_status ember_softmax_loss(const void *logits, int64_t ldz, ember_wdtype ztype,
+                                const void *targets, ember_idtype idtype, const float *weights,
+                                int64_t ignore_index, int mean, int64_t T, int64_t V,
+                                float *loss, float *nll, void *dlogits, int64_t ldd, ember_wdtype dtype,
+                                void *workspace, size_t bytes, unsigned *status, void *stream);
+
+/* Global norm of n gradients, sqrt(sum of g^2 over all of them), and their
+ * clipping by it: out_i = g_i min(1, max_norm / (norm + eps)).
+ *   grads, out: n device pointers each (a host array); tensor i has numel[i]
+ *   contiguous elements (0 allowed) of types[i] (ember_wdtype), in and out;
+ *   out[i] may be grads[i].  norm: one fp32, written.
+ *   max_norm >= 0, eps >= 0.  n = 0 gives the norm 0.
+ * The host arrays are read before the call returns.  An infinite norm makes
+ * the factor 0 (so an infinite element becomes NaN), a NaN makes every
+ * output NaN, as the formula has it; the squares themselves neither overflow
+ * nor underflow.  workspace: ember_clip_workspace_bytes(n). */
+size_t ember_clip_workspace_bytes(int n);
+ember_status ember_grad_norm(int n, const void *const *grads, const int64_t *numel, const int *types,
+                             float *norm, void *workspace, size_t bytes, void *stream);
+ember_status ember_clip_grads(int n, const void *const *grads, void *const *out, const int64_t *numel,
+                              const int *types, float max_norm, float eps, float *norm,
+                              void *workspace, size_t bytes, void *stream);
+
 /* Static description of a status code. */
 const char *ember_status_string(ember_status s);
 

@@ -42,6 +42,10 @@ EXPORTS = (
     "ember_shard_rows", "ember_shard_scale_bytes", "ember_shard_exchange_bytes", "ember_shard_reduce",
     "ember_shard_pack", "ember_shard_update", "ember_column_panels", "ember_set_wait_limit_ns",
     "ember_dense_step_launches",
+    "ember_status_init", "ember_status_read", "ember_rmsnorm", "ember_rmsnorm_quant", "ember_quantize_rows",
+    "ember_dequantize_rows", "ember_rmsnorm_backward_workspace_bytes", "ember_rmsnorm_backward",
+    "ember_matmul_quant_workspace_bytes", "ember_matmul_quant", "ember_softmax_loss_workspace_bytes",
+    "ember_softmax_loss", "ember_clip_workspace_bytes", "ember_grad_norm", "ember_clip_grads",
 )
 
 
@@ -99,6 +103,24 @@ def lib():
             "ember_column_panels": (ip, [vp, ip]),
             "ember_dense_step_launches": (ip, [vp, ip]),
             "ember_set_wait_limit_ns": (st, [vp, ctypes.c_uint64]),
+            # the operators of ops.py
+            "ember_status_init": (st, [vp, vp]),
+            "ember_status_read": (st, [vp, vp]),
+            "ember_rmsnorm": (st, [vp, i64, ip, vp, i64, ip, vp, ip, i64, i64, flt, vp, i64, vp, i64, vp]),
+            "ember_rmsnorm_quant": (st, [vp, i64, ip, vp, i64, ip, vp, ip, i64, i64, flt, vp, i64, vp, i64, vp, vp]),
+            "ember_quantize_rows": (st, [vp, i64, ip, i64, i64, vp, i64, vp, vp]),
+            "ember_dequantize_rows": (st, [vp, i64, vp, i64, i64, vp, i64, ip, vp]),
+            "ember_rmsnorm_backward_workspace_bytes": (sz, [i64, i64]),
+            "ember_rmsnorm_backward": (st, [vp, i64, vp, i64, vp, i64, ip, vp, ip, i64, i64, flt, vp, i64, vp, vp, sz,
+                                            vp]),
+            "ember_matmul_quant_workspace_bytes": (sz, [i64, i64, i64]),
+            "ember_matmul_quant": (st, [vp, i64, vp, vp, i64, vp, i64, i64, i64, vp, i64, ip, vp, sz, vp, vp]),
+            "ember_softmax_loss_workspace_bytes": (sz, [i64]),
+            "ember_softmax_loss": (st, [vp, i64, ip, vp, ip, vp, i64, ip, i64, i64, vp, vp, vp, i64, ip, vp, sz, vp,
+                                        vp]),
+            "ember_clip_workspace_bytes": (sz, [ip]),
+            "ember_grad_norm": (st, [ip, vp, vp, vp, vp, vp, sz, vp]),
+            "ember_clip_grads": (st, [ip, vp, vp, vp, vp, flt, flt, vp, vp, sz, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)

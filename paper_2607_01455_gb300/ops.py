@@ -1,0 +1,333 @@
+"""The operators around a token table's step, on torch tensors: residual
+addition with the RMS norm and its gradients, 8-bit rows and the product of
+8-bit integers, softmax cross-entropy with the gradient of the logits, the
+global gradient norm and clipping.
+
+    ops = Ops()
+    y, h = ops.rmsnorm(x, gain, residual=res)             # hidden states for the head
+    loss, nll, dlogits = ops.softmax_loss(logits, ids)    # what Ember.step_lmhead takes
+    dx, dgain = ops.rmsnorm_backward(dy, h, gain)
+    norm = ops.clip_grads(grads, max_norm=1.0)            # in place
+    wq, ws = ops.quantize_rows(W)                         # the trained table, served in 8 bits
+    q, scales, h = ops.rmsnorm_quant(x, gain, residual=res)
+    logits = ops.matmul_quant(q, scales, wq, ws)
+
+Every computation runs in libember (include/ember.h has each operator's
+definition and limits); this module checks shapes, types and devices, makes
+the outputs that were not passed in, and marshals the arguments.  Matrices
+are 2-D with unit stride along their rows; any row stride is accepted.  Calls
+run on torch's current stream, or on `stream` (a torch stream), whose memory
+their outputs and workspace then come from; a tensor that another stream
+still writes has to be waited for by the caller, as with any torch call.
+"""
+from array import array
+
+import torch
+
+from .ember import (EMBER_BF16, EMBER_ERR_DTYPE, EMBER_ERR_INVALID_ARG, EMBER_F32, EMBER_I32, EMBER_I64, EMBER_OK,
+                    EmberError, _check, _current_stream, lib)
+
+_TYPES = {torch.bfloat16: EMBER_BF16, torch.float32: EMBER_F32}
+_IDS = {torch.int32: EMBER_I32, torch.int64: EMBER_I64}
+
+
+class _Refused(EmberError, ValueError):
+    """A call that the shapes, types or devices of its tensors rule out."""
+
+    def __init__(self, where, why, status=EMBER_ERR_INVALID_ARG):
+        super().__init__(status, f"{where}: {why}")
+
+
+class Ops:
+    """The operators' workspace and sticky status word on one device, for use
+    on one stream (calls on different streams share the workspace: give each
+    stream its own object)."""
+
+    def __init__(self, device="cuda"):
+        dev = torch.device(device)
+        if dev.type != "cuda":
+            raise _Refused("Ops", f"a CUDA device is needed, not {dev}")
+        self.device = torch.device("cuda", torch.cuda.current_device() if dev.index is None else dev.index)
+        self._lib = lib()
+        self._status = self._workspace = None  # made by the first call that needs them, on its stream
+
+    # ---- arguments ----
+
+    def _matrix(self, where, name, t, types=None, shape=None):
+        """(address, row stride) of a 2-D tensor with unit stride along its rows."""
+        if t.device != self.device:
+            raise _Refused(where, f"{name} is on {t.device}, not on {self.device}")
+        if types is not None and t.dtype not in types:
+            raise _Refused(where, f"{name} has type {t.dtype}", EMBER_ERR_DTYPE)
+        if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+            raise _Refused(where, f"{name} has shape {tuple(t.shape)}" + (f", not {shape}" if shape else ", not 2-D"))
+        rows, cols = t.shape
+        sr, sc = t.stride()
+        if cols < 1 or (sc != 1 and cols > 1) or (rows > 1 and sr < cols):
+            raise _Refused(where, f"{name} has strides {t.stride()}: unit stride along rows that do not overlap is needed")
+        return t.data_ptr(), sr if rows > 1 and sr >= cols else cols
+
+    def _vector(self, where, name, t, n, types):
+        if t.device != self.device:
+            raise _Refused(where, f"{name} is on {t.device}, not on {self.device}")
+        if t.dtype not in types:
+            raise _Refused(where, f"{name} has type {t.dtype}", EMBER_ERR_DTYPE)
+        if t.dim() != 1 or t.numel() != n or (n > 1 and t.stride(0) != 1):
+            raise _Refused(where, f"{name} has shape {tuple(t.shape)} and strides {t.stride()}, not {n} in a row")
+        return t.data_ptr()
+
+    def _gain(self, where, gain, D):
+        if gain is None:
+            return None, EMBER_F32
+        return self._vector(where, "gain", gain, D, _TYPES), _TYPES[gain.dtype]
+
+    def _scratch(self, nbytes):
+        w = self._workspace
+        if w is None or w.numel() < nbytes:
+            if w is not None:
+                w.record_stream(torch.cuda.current_stream(self.device))  # calls in flight still use it
+            w = self._workspace = torch.empty(max(nbytes, 1 << 16), dtype=torch.uint8, device=self.device)
+        return w
+
+    def _status_word(self):
+        if self._status is None:
+            self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        return self._status.data_ptr()
+
+    def _on(self, stream):
+        """A context in which torch allocates from the stream that the call runs on."""
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=self.device)
+        return torch.cuda.stream(stream)
+
+    # ---- the norm ----
+
+    def rmsnorm(self, x, gain, residual=None, eps=1e-6, out=None, residual_out=None, stream=None):
+        """(y, h): y = gain s / sqrt(mean s^2 + eps) over the rows of s = x +
+        residual, in x's type, and h = s in the residual's type (None without
+        one).  out may be x, residual_out may be residual."""
+        if stream is not None:
+            with self._on(stream):
+                return self.rmsnorm(x, gain, residual, eps, out, residual_out)
+        w = "rmsnorm"
+        px, ldx = self._matrix(w, "x", x, _TYPES)
+        T, D = x.shape
+        pg, gt = self._gain(w, gain, D)
+        pr, ldr, rt, ph, ldh, h = self._residual(w, residual, residual_out, T, D)
+        y = torch.empty((T, D), dtype=x.dtype, device=self.device) if out is None else out
+        py, ldy = self._matrix(w, "out", y, (x.dtype,), (T, D))
+        _check(self._lib.ember_rmsnorm(px, ldx, _TYPES[x.dtype], pr, ldr, rt, pg, gt, T, D, eps, ph, ldh, py, ldy,
+                                       _current_stream()), w)
+        return y, h
+
+    def _residual(self, where, residual, residual_out, T, D):
+        if residual is None:
+            if residual_out is not None:
+                raise _Refused(where, "residual_out without a residual")
+            return None, 0, EMBER_F32, None, 0, None
+        pr, ldr = self._matrix(where, "residual", residual, _TYPES, (T, D))
+        h = torch.empty((T, D), dtype=residual.dtype, device=self.device) if residual_out is None else residual_out
+        ph, ldh = self._matrix(where, "residual_out", h, (residual.dtype,), (T, D))
+        return pr, ldr, _TYPES[residual.dtype], ph, ldh, h
+
+    def rmsnorm_quant(self, x, gain, residual=None, eps=1e-6, residual_out=None, stream=None):
+        """(q, scales, h): the norm in 8 bits, y about q * scales[:, None]."""
+        if stream is not None:
+            with self._on(stream):
+                return self.rmsnorm_quant(x, gain, residual, eps, residual_out)
+        w = "rmsnorm_quant"
+        px, ldx = self._matrix(w, "x", x, _TYPES)
+        T, D = x.shape
+        pg, gt = self._gain(w, gain, D)
+        pr, ldr, rt, ph, ldh, h = self._residual(w, residual, residual_out, T, D)
+        q, ldq, scales = self._rows8(T, D)
+        _check(self._lib.ember_rmsnorm_quant(px, ldx, _TYPES[x.dtype], pr, ldr, rt, pg, gt, T, D, eps, ph, ldh,
+                                             q.data_ptr(), ldq, scales.data_ptr(), _current_stream()), w)
+        return q, scales, h
+
+    def _rows8(self, T, D):
+        """New 8-bit rows, each on a 16-byte boundary, and their scales."""
+        ld = (D + 15) // 16 * 16
+        q = torch.empty((T, ld), dtype=torch.int8, device=self.device)
+        return q if ld == D else q[:, :D], ld, torch.empty(T, dtype=torch.float32, device=self.device)
+
+    def rmsnorm_backward(self, dy, h, gain, eps=1e-6, dres=None, out=None, stream=None):
+        """(dx, dgain) of the norm at h; dres, what reaches h past the norm, is
+        added to dx.  out may be dy or dres."""
+        if stream is not None:
+            with self._on(stream):
+                return self.rmsnorm_backward(dy, h, gain, eps, dres, out)
+        w = "rmsnorm_backward"
+        ph, ldh = self._matrix(w, "h", h, _TYPES)
+        T, D = h.shape
+        same = (h.dtype,)
+        py, ldy = self._matrix(w, "dy", dy, same, (T, D))
+        pr, ldr = (None, 0) if dres is None else self._matrix(w, "dres", dres, same, (T, D))
+        pg, gt = self._gain(w, gain, D)
+        dx = torch.empty((T, D), dtype=h.dtype, device=self.device) if out is None else out
+        pd, ldd = self._matrix(w, "out", dx, same, (T, D))
+        dgain = torch.empty(D, dtype=torch.float32, device=self.device)
+        ws = self._scratch(self._lib.ember_rmsnorm_backward_workspace_bytes(T, D))
+        _check(self._lib.ember_rmsnorm_backward(py, ldy, ph, ldh, pr, ldr, _TYPES[h.dtype], pg, gt, T, D, eps, pd, ldd,
+                                                dgain.data_ptr(), ws.data_ptr(), ws.numel(), _current_stream()), w)
+        return dx, dgain
+
+    # ---- 8 bits ----
+
+    def quantize_rows(self, x, stream=None):
+        """(q, scales) of a matrix: scales = max |x| / 127 over each row, q = x
+        / scales rounded to nearest even.  Rows of q start on 16 bytes."""
+        if stream is not None:
+            with self._on(stream):
+                return self.quantize_rows(x)
+        w = "quantize_rows"
+        px, ldx = self._matrix(w, "x", x, _TYPES)
+        T, D = x.shape
+        q, ldq, scales = self._rows8(T, D)
+        _check(self._lib.ember_quantize_rows(px, ldx, _TYPES[x.dtype], T, D, q.data_ptr(), ldq, scales.data_ptr(),
+                                             _current_stream()), w)
+        return q, scales
+
+    def dequantize_rows(self, q, scales, dtype=torch.bfloat16, out=None, stream=None):
+        """q * scales[:, None] in `dtype`."""
+        if stream is not None:
+            with self._on(stream):
+                return self.dequantize_rows(q, scales, dtype, out)
+        w = "dequantize_rows"
+        pq, ldq = self._matrix(w, "q", q, (torch.int8,))
+        T, D = q.shape
+        ps = self._vector(w, "scales", scales, T, (torch.float32,))
+        if dtype not in _TYPES:
+            raise _Refused(w, f"an output of type {dtype}", EMBER_ERR_DTYPE)
+        y = torch.empty((T, D), dtype=dtype, device=self.device) if out is None else out
+        py, ldy = self._matrix(w, "out", y, (dtype,), (T, D))
+        _check(self._lib.ember_dequantize_rows(pq, ldq, ps, T, D, py, ldy, _TYPES[dtype], _current_stream()), w)
+        return y
+
+    def matmul_quant(self, xq, xs, wq, ws, dtype=torch.bfloat16, out=None, stream=None):
+        """out[t][v] = xs[t] ws[v] sum_k xq[t][k] wq[v][k] in `dtype`; xq (T x
+        K) and wq (V x K) int8, xs and ws fp32."""
+        if stream is not None:
+            with self._on(stream):
+                return self.matmul_quant(xq, xs, wq, ws, dtype, out)
+        w = "matmul_quant"
+        px, ldx = self._matrix(w, "xq", xq, (torch.int8,))
+        T, K = xq.shape
+        pw, ldw = self._matrix(w, "wq", wq, (torch.int8,))
+        V = wq.shape[0]
+        if wq.shape[1] != K:
+            raise _Refused(w, f"rows of {K} and of {wq.shape[1]} values")
+        pxs = self._vector(w, "xs", xs, T, (torch.float32,))
+        pws = self._vector(w, "ws", ws, V, (torch.float32,))
+        if dtype not in _TYPES:
+            raise _Refused(w, f"an output of type {dtype}", EMBER_ERR_DTYPE)
+        o = torch.empty((T, V), dtype=dtype, device=self.device) if out is None else out
+        po, ldo = self._matrix(w, "out", o, (dtype,), (T, V))
+        work = self._scratch(self._lib.ember_matmul_quant_workspace_bytes(T, V, K))
+        _check(self._lib.ember_matmul_quant(px, ldx, pxs, pw, ldw, pws, T, V, K, po, ldo, _TYPES[dtype],
+                                            work.data_ptr(), work.numel(), self._status_word(),
+                                            _current_stream()), w)
+        return o
+
+    # ---- the loss ----
+
+    def softmax_loss(self, logits, targets, weights=None, ignore_index=-100, reduction="mean", grad=True,
+                     grad_dtype=None, out=None, stream=None):
+        """(loss, nll, dlogits): softmax cross-entropy of T tokens over V
+        entries.  nll per token, loss = sum w nll (over the counted tokens'
+        number with reduction="mean"), dlogits the loss's gradient in
+        grad_dtype (the logits' type by default), None with grad=False.
+        out may be logits."""
+        if stream is not None:
+            with self._on(stream):
+                return self.softmax_loss(logits, targets, weights, ignore_index, reduction, grad, grad_dtype, out)
+        w = "softmax_loss"
+        pz, ldz = self._matrix(w, "logits", logits, _TYPES)
+        T, V = logits.shape
+        py = self._vector(w, "targets", targets, T, _IDS)
+        pw = None if weights is None else self._vector(w, "weights", weights, T, (torch.float32,))
+        if reduction not in ("mean", "sum"):
+            raise _Refused(w, f"reduction {reduction!r} is neither 'mean' nor 'sum'")
+        dt = grad_dtype or (logits.dtype if out is None else out.dtype)
+        if dt not in _TYPES:
+            raise _Refused(w, f"a gradient of type {dt}", EMBER_ERR_DTYPE)
+        d, pd, ldd = None, None, 0
+        if grad:
+            # rows of the gradient start where those of the logits do in a group
+            # of 16 bytes, so that both take wide accesses
+            ld = ldz if ldz < V + 64 else (V + 7) // 8 * 8
+            d = torch.empty_strided((T, V), (ld, 1), dtype=dt, device=self.device) if out is None else out
+            pd, ldd = self._matrix(w, "out", d, (dt,), (T, V))
+        loss = torch.empty((), dtype=torch.float32, device=self.device)
+        nll = torch.empty(T, dtype=torch.float32, device=self.device)
+        work = self._scratch(self._lib.ember_softmax_loss_workspace_bytes(T))
+        _check(self._lib.ember_softmax_loss(pz, ldz, _TYPES[logits.dtype], py, _IDS[targets.dtype], pw, ignore_index,
+                                            int(reduction == "mean"), T, V, loss.data_ptr(), nll.data_ptr(), pd, ldd,
+                                            _TYPES[dt], work.data_ptr(), work.numel(), self._status_word(),
+                                            _current_stream()), w)
+        return loss, nll, d
+
+    # ---- gradients ----
+
+    def _list(self, where, tensors, out):
+        """The host arrays of a call over many tensors: addresses, sizes, types."""
+        dev = self.device
+        for t in tensors:
+            if t.device != dev or not t.is_contiguous():
+                raise _Refused(where, f"a gradient of shape {tuple(t.shape)}, strides {t.stride()} on {t.device}: "
+                                      f"contiguous tensors on {dev} are needed")
+        try:
+            types = array("i", [_TYPES[t.dtype] for t in tensors])
+        except KeyError as e:
+            raise _Refused(where, f"a gradient of type {e.args[0]}", EMBER_ERR_DTYPE) from None
+        numel = array("q", [t.numel() for t in tensors])
+        ptrs = array("Q", [t.data_ptr() for t in tensors])
+        outs = ptrs
+        if out is not None:
+            if len(out) != len(tensors):
+                raise _Refused(where, f"{len(out)} outputs for {len(tensors)} gradients")
+            for t, o in zip(tensors, out):
+                if o.dtype != t.dtype or o.shape != t.shape or o.device != dev or not o.is_contiguous():
+                    raise _Refused(where, f"an output of shape {tuple(o.shape)}, type {o.dtype} for a gradient of "
+                                          f"shape {tuple(t.shape)}, type {t.dtype}")
+            outs = array("Q", [o.data_ptr() for o in out])
+        return ptrs, outs, numel, types
+
+    def grad_norm(self, tensors, stream=None):
+        """sqrt(sum of squares over all tensors), a scalar on the device."""
+        if stream is not None:
+            with self._on(stream):
+                return self.grad_norm(tensors)
+        w = "grad_norm"
+        tensors = list(tensors)
+        ptrs, _, numel, types = self._list(w, tensors, None)
+        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        n = len(tensors)
+        work = self._scratch(self._lib.ember_clip_workspace_bytes(n))
+        _check(self._lib.ember_grad_norm(n, ptrs.buffer_info()[0], numel.buffer_info()[0], types.buffer_info()[0],
+                                         norm.data_ptr(), work.data_ptr(), work.numel(), _current_stream()), w)
+        return norm
+
+    def clip_grads(self, tensors, max_norm, out=None, eps=1e-6, stream=None):
+        """Multiplies every gradient by min(1, max_norm / (norm + eps)), in
+        place or into the tensors of `out`; returns the norm before clipping,
+        a scalar on the device."""
+        if stream is not None:
+            with self._on(stream):
+                return self.clip_grads(tensors, max_norm, out, eps)
+        w = "clip_grads"
+        tensors = list(tensors)
+        ptrs, outs, numel, types = self._list(w, tensors, out)
+        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        n = len(tensors)
+        work = self._scratch(self._lib.ember_clip_workspace_bytes(n))
+        _check(self._lib.ember_clip_grads(n, ptrs.buffer_info()[0], outs.buffer_info()[0], numel.buffer_info()[0],
+                                          types.buffer_info()[0], max_norm, eps, norm.data_ptr(), work.data_ptr(),
+                                          work.numel(), _current_stream()), w)
+        return norm
+
+    def device_status(self, stream=None):
+        """Synchronises; returns (and clears) the sticky status: EMBER_OK,
+        EMBER_ERR_ID_OUT_OF_RANGE (a target) or EMBER_ERR_TIMEOUT."""
+        return self._lib.ember_status_read(self._status_word(),
+                                           _current_stream() if stream is None else getattr(stream, "cuda_stream", stream))
