@@ -58,18 +58,17 @@
 // wall time); a wait that gives up sets the sticky timeout flag, stops every
 // role, lets the copies and MMAs already issued finish (those teardown waits
 // keep the fixed 2 s limit), frees the tensor memory and returns.
-#include <cuda.h>
-#include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-#include <mutex>
-
 #include "ember_device.cuh"
 #include "ember_internal.h"
+#include "ember_tc.cuh"
 
 namespace ember {
 namespace {
+
+using namespace tc;
 
 constexpr int kBM = 128;                    // accumulator rows per CTA (half the pair's UMMA M)
 constexpr int kPairM = 2 * kBM;             // UMMA M of the pair
@@ -86,7 +85,6 @@ constexpr int kAccCols = kBN;               // fp32 accumulator columns per tile
 constexpr int kTmemCols = 2 * kAccCols;     // two accumulators
 constexpr int kLmThreads = 256;
 constexpr int kEpiWarp0 = 4;
-constexpr uint64_t kWaitNs = 2000000000ull;  // 2 s
 // Column blocks per band of the tile order (see tile_of).
 constexpr int kLmBand = 16;
 
@@ -109,87 +107,6 @@ constexpr int kStoreBytes = 4 * kStoreBufs * kStoreBlockBytes;
 constexpr size_t kLmSmemBytes = 1024 + (size_t)kStages * kStageBytes + kStoreBytes + sizeof(LmSmemTail);
 static_assert(kLmSmemBytes <= 232448, "over the 227 KiB of shared memory a CTA may use");
 
-__device__ __forceinline__ uint32_t smem_addr(const void *p)
-{
-    return (uint32_t)__cvta_generic_to_shared(p);
-}
-
-__device__ __forceinline__ uint64_t now_ns()
-{
-    uint64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
-                 : "memory");
-}
-
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-
-// Wait for the phase of parity `parity` of `bar` to complete.  Gives up when
-// another role has aborted or after limit_ns (the handle's wait limit);
-// returns false then.
-__device__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *abort, uint64_t limit_ns)
-{
-    if (mbar_test(bar, parity))
-        return true;
-    // try_wait may suspend the thread for a while before it reports "not
-    // yet", so the clock and the abort word are checked after every try
-    const uint64_t t0 = now_ns();
-    for (;;) {
-        if (mbar_test(bar, parity))
-            return true;
-        if (*abort)
-            return false;
-        if (now_ns() - t0 > limit_ns)
-            return false;
-    }
-}
-
-// Same, for teardown: no abort check, only the fixed limit kWaitNs (the
-// copies and MMAs already issued are waited for even when the main-loop
-// limit was made short).
-__device__ bool mbar_wait_final(uint32_t bar, uint32_t parity)
-{
-    const uint64_t t0 = now_ns();
-    while (!mbar_test(bar, parity))
-        if (now_ns() - t0 > kWaitNs)
-            return false;
-    return true;
-}
-
-// L2 eviction policies for the TMA loads (createpolicy; fraction 1.0).
-__device__ __forceinline__ uint64_t l2_policy(int kind)
-{
-    uint64_t p;
-    if (kind == 1)
-        asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
-    else if (kind == 2)
-        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
-    else
-        asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
-    return p;
-}
-
 // G block of 32 columns x 32 rows from shared memory to global, clipped at
 // the edges of G by the tensor map; one bulk group per call.
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int x, int y, uint64_t pol)
@@ -207,9 +124,6 @@ __device__ __forceinline__ void tma_store_wait_read()
     asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ void tma_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
 // Shared-memory matrix descriptor of tcgen05.mma for an MN-major operand
 // with the 128-byte swizzle: start address, 10 KiB between 64-element blocks
@@ -235,26 +149,6 @@ constexpr uint32_t kInstrDesc = (1u << 4)               // D: f32
                                 | ((uint32_t)(kBN >> 3) << 17)
                                 | ((uint32_t)(kPairM >> 4) << 24);
 
-// 32 consecutive fp32 accumulator columns of this thread's lane.
-__device__ __forceinline__ void tmem_load32(uint32_t taddr, float (&v)[32])
-{
-    uint32_t r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-          "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
-          "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int e = 0; e < 32; ++e)
-        v[e] = __uint_as_float(r[e]);
-}
-
 // Named barrier 1 over the 128 epilogue threads.
 __device__ __forceinline__ void epi_bar() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
@@ -274,61 +168,6 @@ __device__ __forceinline__ bool epi_bar_any(bool c)
     return r != 0;
 }
 
-__device__ void set_timeout(volatile int *abort, unsigned *flags)
-{
-    *abort = 1;
-    atomicOr(flags, kFlagTimeout);
-}
-
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_id()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%clusterid.x;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_count()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%nclusterid.x;" : "=r"(r));
-    return r;
-}
-// Every thread of every CTA of the cluster: arrive, then wait for all.
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-// Address of the same shared-memory variable in CTA `rank` of the cluster.
-__device__ __forceinline__ uint32_t mapa_rank(uint32_t addr, uint32_t rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)
-{
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-
-// One 64 x 64 box into this CTA's shared memory; its bytes complete on the
-// barrier `bar` (a cluster address: the leader's barrier for both CTAs).
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar,
-                                            uint64_t pol)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
-        ".L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar), "l"(pol)
-        : "memory");
-}
-
 __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t acc)
 {
     asm volatile(
@@ -337,22 +176,6 @@ __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a, uint64_t b
         "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
         "l"(a), "l"(b), "r"(kInstrDesc), "r"(acc)
         : "memory");
-}
-
-// Arrive on the barrier at `bar`'s offset in both CTAs of the pair once the
-// MMAs issued so far by this thread have completed.
-__device__ __forceinline__ void mma_commit_mc(uint32_t bar)
-{
-    asm volatile(
-        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-        "h"((uint16_t)3)
-        : "memory");
-}
-
-__device__ __forceinline__ void mma_commit(uint32_t bar)
-{
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
-                 : "memory");
 }
 
 // Pair tile gt -> (row block mb of this CTA, column block nb).  Column
@@ -619,21 +442,6 @@ k_lmhead_grad(const __grid_constant__ CUtensorMap tm_dl, const __grid_constant__
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols)
                      : "memory");
     }
-}
-
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
-{
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
-    static std::once_flag once;
-    std::call_once(once, [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) ==
-                cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-    });
-    return fn;
 }
 
 // G, V x D fp32 row-major, stored as 32 x 32 boxes with the 128-byte swizzle.

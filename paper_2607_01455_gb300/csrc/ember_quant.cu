@@ -4,12 +4,32 @@
 //
 // the logits of a head whose table is kept in 8 bits (ember_quantize_rows)
 // and whose hidden states the norm wrote in 8 bits (ember_rmsnorm_quant).
+//
+// Three kernels, by the number of tokens and the rows' alignment:
+//   k_mm_few   up to kFewTokens tokens: the table is read once, the products
+//              by dp4a; bound by HBM.
+//   k_mm_tc    more tokens: tcgen05 on pairs of CTAs; bound by HBM up to
+//              about 128 tokens, by the tensor cores beyond.
+//   k_mm_any   tables whose rows do not start on 16 bytes.
+//
+// GB300's tensor cores have no fast 8-bit integer form, but an 8-bit integer
+// is an fp16 number: k_mm_tc widens the table's tiles on their way into
+// tensor memory and multiplies in fp16 with fp32 sums.  Products of two
+// 8-bit integers and sums of them below 2^24 are exact in fp32, so the result
+// is the integer one as long as sum_k |xq wq| < 2^24 (always for K <= 1024,
+// and for hidden states and tables in use far beyond); past that a sum is
+// rounded like any fp32 sum.
 #include "ember_rows.cuh"
+#include "ember_tc.cuh"
+
+#include <cuda_fp16.h>
 
 namespace ember {
 namespace {
 
 using namespace rows;
+
+constexpr int64_t kMaxMmRows = INT32_MAX - 1024;  // row numbers of a last tile stay within 32 bits
 
 struct MmArgs {
     const int8_t *xq, *wq;
@@ -78,6 +98,627 @@ __global__ void __launch_bounds__(256) k_mm_any(MmArgs a, int obf16, unsigned vb
     }
 }
 
+
+// ---------------------------------------------------------------------------
+// Few tokens.  The tokens' rows sit in shared memory, zero-padded to whole
+// 512-byte slabs; a warp takes kFewRows rows of the table at a time, 16 bytes
+// of each row per lane and slab, so that every 16 bytes of x are read from
+// shared memory once for kFewRows rows.  The lanes' integer sums are joined by
+// a transposed butterfly: kFewRows TN totals for about as many shuffles.
+// ---------------------------------------------------------------------------
+constexpr int kFewTokens = 8;
+constexpr int kFewRows = 4;
+constexpr int kFewThreads = 256;
+constexpr size_t kFewSmem = 100 << 10;  // two CTAs per SM
+
+template <int R>
+__device__ __forceinline__ int warp_isum_transposed(int (&v)[R], int lane, int &index)
+{
+    constexpr int kLog = R >= 32 ? 5 : R >= 16 ? 4 : R >= 8 ? 3 : R >= 4 ? 2 : R >= 2 ? 1 : 0;
+    static_assert((1 << kLog) == R, "a power of two up to 32");
+    index = 0;
+#pragma unroll
+    for (int s = 0; s < kLog; ++s) {
+        const int o = 16 >> s;
+        const int h = R >> (s + 1);
+        const bool hi = (lane & o) != 0;
+#pragma unroll
+        for (int m = 0; m < h; ++m) {
+            const int send = hi ? v[m] : v[m + h];
+            const int keep = hi ? v[m + h] : v[m];
+            v[m] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+        }
+        if (hi)
+            index += h;
+    }
+#pragma unroll
+    for (int o = 16 >> kLog; o >= 1; o >>= 1)
+        v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    return v[0];
+}
+
+__device__ __forceinline__ int4 ldg_stream(const int8_t *p)
+{
+    int4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.s32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p));
+    return v;
+}
+__device__ __forceinline__ int dot16(int4 a, int4 b, int c)
+{
+    return __dp4a(a.w, b.w, __dp4a(a.z, b.z, __dp4a(a.y, b.y, __dp4a(a.x, b.x, c))));
+}
+
+template <int TN>
+__global__ void __launch_bounds__(kFewThreads, 2) k_mm_few(MmArgs a, int obf16, int kpad)
+{
+    extern __shared__ __align__(16) int8_t sx[];  // [TN][kpad]
+    const int lane = threadIdx.x & 31;
+    dev::grid_dep_wait();
+    dev::grid_dep_launch();
+    for (int t = 0; t < TN; ++t) {
+        const int8_t *row = a.xq + t * a.ldx;
+        const bool on = t < a.T;
+        if (on && (uintptr_t)row % 16 == 0) {
+            for (int k = threadIdx.x * 16; k < kpad; k += kFewThreads * 16) {
+                int4 v = make_int4(0, 0, 0, 0);
+                if (k + 16 <= a.K)
+                    v = *reinterpret_cast<const int4 *>(row + k);
+                else
+                    for (int e = 0; k + e < a.K; ++e)
+                        reinterpret_cast<int8_t *>(&v)[e] = row[k + e];
+                *reinterpret_cast<int4 *>(sx + t * kpad + k) = v;
+            }
+        } else
+            for (int k = threadIdx.x; k < kpad; k += kFewThreads)
+                sx[t * kpad + k] = on && k < a.K ? row[k] : 0;
+    }
+    __syncthreads();
+    const int whole = a.K / 16 * 16;  // up to here 16 bytes at once lie inside a row
+    const int64_t nquads = (a.V + kFewRows - 1) / kFewRows;
+    const int64_t step = (int64_t)gridDim.x * (kFewThreads / 32);
+    for (int64_t q = (int64_t)blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5); q < nquads; q += step) {
+        int acc[kFewRows * TN];  // [row][token]
+#pragma unroll
+        for (int e = 0; e < kFewRows * TN; ++e)
+            acc[e] = 0;
+        const int8_t *w[kFewRows];
+#pragma unroll
+        for (int r = 0; r < kFewRows; ++r) {
+            const int64_t v = q * kFewRows + r;
+            w[r] = a.wq + (v < a.V ? v : a.V - 1) * a.ldw;
+        }
+#pragma unroll 2
+        for (int k = lane * 16; k < whole; k += 512) {
+            int4 c[kFewRows];
+#pragma unroll
+            for (int r = 0; r < kFewRows; ++r)
+                c[r] = ldg_stream(w[r] + k);
+#pragma unroll
+            for (int t = 0; t < TN; ++t) {
+                const int4 x = *reinterpret_cast<const int4 *>(sx + t * kpad + k);
+#pragma unroll
+                for (int r = 0; r < kFewRows; ++r)
+                    acc[r * TN + t] = dot16(c[r], x, acc[r * TN + t]);
+            }
+        }
+        if (whole + lane < a.K) {  // the last, at most 15 values of a row, one per lane
+#pragma unroll
+            for (int r = 0; r < kFewRows; ++r)
+#pragma unroll
+                for (int t = 0; t < TN; ++t)
+                    acc[r * TN + t] += (int)w[r][whole + lane] * (int)sx[t * kpad + whole + lane];
+        }
+        int index;
+        const int sum = warp_isum_transposed<kFewRows * TN>(acc, lane, index);
+        const int64_t v = q * kFewRows + index / TN;
+        const int t = index % TN;
+        if (lane % (32 / (kFewRows * TN)) == 0 && v < a.V && t < a.T)
+            store_out(a.out, obf16, t * a.ldo + v, (float)sum * a.xs[t] * a.ws[v]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Many tokens, on the tensor cores.  A pair of CTAs multiplies 256 rows of the
+// table (the M of tcgen05.mma.cta_group::2, 128 rows in each CTA) by N tokens.
+// Per block of 128 along K each CTA
+//   - gets its 128 rows of the table as they are, 16 KiB of 8-bit integers, by
+//     TMA into 128-byte swizzled shared memory;
+//   - widens them to fp16 in registers (a thread per row, 128 values) and
+//     stores them in tensor memory as the A operand, 64 columns: shared memory
+//     sees 8 bits per value of the table, not 8 + 16 + 16;
+//   - gets its half of the tokens' block, already fp16 (k_widen writes them
+//     once per call), by TMA.
+// Roles (512 threads per CTA, one CTA per SM, persistent over tiles):
+//   warp 0      issues the TMA loads
+//   warp 1      allocates tensor memory; in the even CTA issues the MMAs
+//   warps 4-7   epilogue: scales and stores an accumulator (two of them, so
+//               that it overlaps the next tile's MMAs)
+//   warps 8-15  widen: two sets of four warps take the blocks in turn
+// Every wait is bounded; one that gives up sets the timeout flag, stops every
+// role, and the kernel returns after its copies and MMAs in flight are done.
+// ---------------------------------------------------------------------------
+using namespace tc;
+
+constexpr int kTcRows = 128;        // rows of the table per CTA
+constexpr int kTcK = 128;           // block along K
+constexpr int kTcThreads = 512;
+constexpr int kTcMaxN = 192;        // two accumulators and two A slots fill tensor memory
+constexpr int kTcMaxStages = 8, kTcMaxSlots = 4;
+constexpr int kTcWBytes = kTcRows * kTcK;
+constexpr int kTcSlotCols = kTcK / 2;  // fp16 pairs
+constexpr size_t kTcSmem = 227 << 10;
+
+struct TcTail {
+    uint64_t wfull[kTcMaxStages];   // each CTA: its rows of the table landed
+    uint64_t wempty[kTcMaxStages];  // each CTA: read by its four widening warps
+    uint64_t bfull[kTcMaxStages];   // even CTA: both halves of the tokens landed
+    uint64_t bempty[kTcMaxStages];  // each CTA: the MMAs of the stage are done
+    uint64_t afull[kTcMaxSlots];    // even CTA: both CTAs' A slots written
+    uint64_t aempty[kTcMaxSlots];   // each CTA: the MMAs of the slot are done
+    uint64_t tfull[2], tempty[2];   // accumulators, as in the LM-head kernel
+    uint64_t drain;
+    uint32_t tmem_base;
+    int abort;
+};
+
+struct TcArgs {
+    const float *xs, *ws;
+    void *out;
+    unsigned *flags;
+    int64_t ldo;
+    int T, V, K;
+    int N, ntb, stages, slots, obf16;
+    uint32_t idesc;
+    uint64_t wait_ns;
+};
+
+// Shared-memory descriptor of a K-major operand with 128-byte swizzled rows
+// of 64 fp16: 1 KiB between groups of 8 rows, descriptor version 1.
+__device__ __forceinline__ uint64_t k_major_sw128_desc(uint32_t saddr)
+{
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)2 << 61;
+}
+
+__device__ __forceinline__ void mma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_store32(uint32_t taddr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+        "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+        : "memory");
+}
+
+// Four 8-bit integers as two pairs of fp16.  A byte with its sign bit flipped
+// is q + 128 in [0, 255]; behind the byte 0x64 it is the fp16 number 1024 + q +
+// 128, exact, and one subtraction leaves q.
+__device__ __forceinline__ uint2 widen4(unsigned q)
+{
+    const unsigned b = q ^ 0x80808080u;
+    const __half2 bias = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
+    const unsigned lo = __byte_perm(b, 0x64646464u, 0x4140), hi = __byte_perm(b, 0x64646464u, 0x4342);
+    const __half2 l = __hsub2(*reinterpret_cast<const __half2 *>(&lo), bias);
+    const __half2 h = __hsub2(*reinterpret_cast<const __half2 *>(&hi), bias);
+    return make_uint2(*reinterpret_cast<const unsigned *>(&l), *reinterpret_cast<const unsigned *>(&h));
+}
+
+// The tokens as fp16, rows of kp (a multiple of 8) values, zeros behind K.
+__global__ void __launch_bounds__(256) k_widen(const int8_t *__restrict__ xq, int64_t ldx, int K, int kp,
+                                               uint4 *__restrict__ xh)
+{
+    const int64_t t = blockIdx.x;
+    const int8_t *row = xq + t * ldx;
+    dev::grid_dep_wait();
+    dev::grid_dep_launch();
+    const bool wide = (uintptr_t)row % 8 == 0;
+    for (int k = threadIdx.x * 8; k < kp; k += 256 * 8) {
+        uint2 q = make_uint2(0, 0);
+        if (wide && k + 8 <= K)
+            q = *reinterpret_cast<const uint2 *>(row + k);
+        else
+            for (int e = 0; e < 8 && k + e < K; ++e)
+                reinterpret_cast<int8_t *>(&q)[e] = row[k + e];
+        const uint2 a = widen4(q.x), b = widen4(q.y);
+        xh[(t * kp + k) / 8] = make_uint4(a.x, a.y, b.x, b.y);
+    }
+}
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__global__ void __launch_bounds__(kTcThreads, 1)
+k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const TcArgs a)
+{
+    extern __shared__ unsigned char tc_smem_raw[];
+    unsigned char *smem =
+        reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(tc_smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int b_box = a.N / 2 * 128;  // N / 2 tokens x 64 fp16
+    const int stage_bytes = kTcWBytes + 2 * b_box;
+    TcTail *tail = reinterpret_cast<TcTail *>(smem + (size_t)a.stages * stage_bytes);
+    volatile int *abort = &tail->abort;
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank();
+    const bool leader = rank == 0;
+    const int ntiles = (a.V + 2 * kTcRows - 1) / (2 * kTcRows) * a.ntb;
+    const int kblocks = (a.K + kTcK - 1) / kTcK;
+    const int tile0 = (int)cluster_id(), tstep = (int)cluster_count();
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < a.stages; ++s) {
+            mbar_init(smem_addr(&tail->wfull[s]), 1);
+            mbar_init(smem_addr(&tail->wempty[s]), 4);
+            mbar_init(smem_addr(&tail->bfull[s]), 1);
+            mbar_init(smem_addr(&tail->bempty[s]), 1);
+        }
+        for (int s = 0; s < a.slots; ++s) {
+            mbar_init(smem_addr(&tail->afull[s]), 8);  // four warps in each CTA
+            mbar_init(smem_addr(&tail->aempty[s]), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(smem_addr(&tail->tfull[s]), 1);
+            mbar_init(smem_addr(&tail->tempty[s]), 8);
+        }
+        mbar_init(smem_addr(&tail->drain), 1);
+        tail->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_w)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_x)) : "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                         smem_addr(&tail->tmem_base)),
+                     "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // no peer may signal this CTA's barriers before they are initialised
+    tc_fence_after();
+    const uint32_t tmem = tail->tmem_base;
+    const uint32_t slot0 = tmem + 2 * a.N;
+    dev::grid_dep_wait();
+    dev::grid_dep_launch();
+
+    if (warp == 0 && lane == 0) {
+        // ---------------- TMA producer (both CTAs) ----------------
+        int stage = 0;
+        uint32_t phase = 0;
+        uint32_t issued = 0, parity = 0;  // a bit per stage: a copy was issued, the parity of its last phase
+        asm volatile("fence.proxy.async.global;" ::: "memory");  // the tokens were written by plain stores
+        const uint64_t pol_w = l2_policy(a.ntb > 1 ? 0 : 2);  // the table streams when every tile is read once
+        const uint64_t pol_x = l2_policy(1);
+        bool ok = true;
+        for (int tile = tile0; tile < ntiles && ok; tile += tstep) {
+            const int vrow = (tile / a.ntb * 2 + rank) * kTcRows;
+            const int trow = tile % a.ntb * a.N + rank * (a.N / 2);
+            for (int kb = 0; kb < kblocks; ++kb) {
+                if (!mbar_wait(smem_addr(&tail->wempty[stage]), phase ^ 1u, abort, a.wait_ns) ||
+                    !mbar_wait(smem_addr(&tail->bempty[stage]), phase ^ 1u, abort, a.wait_ns)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t wbar = smem_addr(&tail->wfull[stage]);
+                const uint32_t bbar = smem_addr(&tail->bfull[stage]);
+                mbar_expect_tx(wbar, kTcWBytes);
+                if (leader)
+                    mbar_expect_tx(bbar, 4 * b_box);  // both CTAs' halves, two boxes each
+                issued |= 1u << stage;
+                parity = (parity & ~(1u << stage)) | phase << stage;
+                const uint32_t dst = smem_addr(smem + (size_t)stage * stage_bytes);
+                const uint32_t lead = mapa_rank(bbar, 0);
+                tma_load_2d(dst, &tm_w, kb * kTcK, vrow, wbar, pol_w);
+                tma_load_2d(dst + kTcWBytes, &tm_x, kb * kTcK, trow, lead, pol_x);
+                tma_load_2d(dst + kTcWBytes + b_box, &tm_x, kb * kTcK + 64, trow, lead, pol_x);
+                if (++stage == a.stages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+        }
+        if (!ok)
+            set_timeout(abort, a.flags);
+        // copies already issued land before the pair meets at the last barrier
+        for (int s = 0; s < a.stages; ++s)
+            if (issued >> s & 1u) {
+                mbar_wait_final(smem_addr(&tail->wfull[s]), parity >> s & 1u);
+                if (leader)
+                    mbar_wait_final(smem_addr(&tail->bfull[s]), parity >> s & 1u);
+            }
+    } else if (warp == 1 && lane == 0 && leader) {
+        // ---------------- MMA issuer (even CTA) ----------------
+        int stage = 0, slot = 0, acc = 0;
+        uint32_t phase = 0, aphase = 0, acc_phase = 0;
+        bool ok = true;
+        for (int tile = tile0; tile < ntiles && ok; tile += tstep) {
+            if (!mbar_wait(smem_addr(&tail->tempty[acc]), acc_phase ^ 1u, abort, a.wait_ns)) {
+                ok = false;
+                break;
+            }
+            const uint32_t d_tmem = tmem + (uint32_t)(acc * a.N);
+            for (int kb = 0; kb < kblocks; ++kb) {
+                if (!mbar_wait(smem_addr(&tail->bfull[stage]), phase, abort, a.wait_ns) ||
+                    !mbar_wait(smem_addr(&tail->afull[slot]), aphase, abort, a.wait_ns)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t b_base = smem_addr(smem + (size_t)stage * stage_bytes) + kTcWBytes;
+                const uint32_t a_base = slot0 + (uint32_t)(slot * kTcSlotCols);
+#pragma unroll
+                for (int k = 0; k < kTcK / 16; ++k)
+                    mma_f16_ta(d_tmem, a_base + k * 8, k_major_sw128_desc(b_base + (k >> 2) * b_box + (k & 3) * 32),
+                               a.idesc, (kb | k) != 0);
+                mma_commit_mc(smem_addr(&tail->bempty[stage]));
+                mma_commit_mc(smem_addr(&tail->aempty[slot]));
+                if (++stage == a.stages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+                if (++slot == a.slots) {
+                    slot = 0;
+                    aphase ^= 1u;
+                }
+            }
+            if (!ok)
+                break;
+            mma_commit_mc(smem_addr(&tail->tfull[acc]));
+            if (++acc == 2) {
+                acc = 0;
+                acc_phase ^= 1u;
+            }
+        }
+        if (!ok)
+            set_timeout(abort, a.flags);
+        mma_commit(smem_addr(&tail->drain));
+        mbar_wait_final(smem_addr(&tail->drain), 0);
+    } else if (warp >= 8) {
+        // ---------------- widening: the table's rows into tensor memory ----------------
+        const int q = warp & 3;
+        const int set = (warp - 8) >> 2;
+        const int r = q * 32 + lane;
+        const uint32_t lanes = (uint32_t)(q * 32) << 16;
+        int stage = 0, slot = 0;
+        uint32_t phase = 0, aphase = 0;
+        int turn = 0;
+        bool ok = true;
+        for (int tile = tile0; tile < ntiles && ok; tile += tstep) {
+            for (int kb = 0; kb < kblocks; ++kb) {
+                if (turn == set) {
+                    ok = mbar_wait(smem_addr(&tail->wfull[stage]), phase, abort, a.wait_ns);
+                    if (!__all_sync(0xffffffffu, ok)) {
+                        ok = false;
+                        break;
+                    }
+                    const unsigned char *row = smem + (size_t)stage * stage_bytes + r * 128;
+                    uint4 raw[8];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        raw[c] = *reinterpret_cast<const uint4 *>(row + ((c ^ (r & 7)) << 4));
+                    __syncwarp();
+                    if (lane == 0)
+                        mbar_arrive(smem_addr(&tail->wempty[stage]));
+                    ok = mbar_wait(smem_addr(&tail->aempty[slot]), aphase ^ 1u, abort, a.wait_ns);
+                    if (!__all_sync(0xffffffffu, ok)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t w[32];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const uint4 v = raw[h * 4 + c];
+                            const uint2 x0 = widen4(v.x), x1 = widen4(v.y), x2 = widen4(v.z), x3 = widen4(v.w);
+                            w[c * 8] = x0.x;
+                            w[c * 8 + 1] = x0.y;
+                            w[c * 8 + 2] = x1.x;
+                            w[c * 8 + 3] = x1.y;
+                            w[c * 8 + 4] = x2.x;
+                            w[c * 8 + 5] = x2.y;
+                            w[c * 8 + 6] = x3.x;
+                            w[c * 8 + 7] = x3.y;
+                        }
+                        tmem_store32(slot0 + (uint32_t)(slot * kTcSlotCols + h * 32) + lanes, w);
+                    }
+                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0)
+                        mbar_arrive_cluster(mapa_rank(smem_addr(&tail->afull[slot]), 0));
+                }
+                turn ^= 1;
+                if (++stage == a.stages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+                if (++slot == a.slots) {
+                    slot = 0;
+                    aphase ^= 1u;
+                }
+            }
+        }
+        if (!ok && lane == 0 && !*abort)
+            set_timeout(abort, a.flags);
+    } else if (warp >= 4) {
+        // ---------------- epilogue (both CTAs) ----------------
+        const int q = warp - 4;
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        for (int tile = tile0; tile < ntiles; tile += tstep) {
+            const bool ok = mbar_wait(smem_addr(&tail->tfull[acc]), acc_phase, abort, a.wait_ns);
+            if (!__all_sync(0xffffffffu, ok)) {
+                if (lane == 0 && !*abort)
+                    set_timeout(abort, a.flags);
+                break;
+            }
+            tc_fence_after();
+            const int v = (tile / a.ntb * 2 + rank) * kTcRows + q * 32 + lane;
+            const int t0 = tile % a.ntb * a.N;
+            const float ws = v < a.V ? a.ws[v] : 0.f;
+            for (int ch = 0; ch < a.N / 32 && t0 + ch * 32 < a.T; ++ch) {
+                const int tc0 = t0 + ch * 32;
+                const float xs = tc0 + lane < a.T ? a.xs[tc0 + lane] : 0.f;
+                float d[32];
+                tmem_load32(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * a.N + ch * 32), d);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const float x = __shfl_sync(0xffffffffu, xs, e);
+                    if (tc0 + e < a.T && v < a.V)
+                        store_out(a.out, a.obf16, (int64_t)(tc0 + e) * a.ldo + v, d[e] * x * ws);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive_cluster(mapa_rank(smem_addr(&tail->tempty[acc]), 0));
+            if (++acc == 2) {
+                acc = 0;
+                acc_phase ^= 1u;
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // the pair's MMAs and arrivals are over on both sides
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// R x C elements of `size` bytes with a row stride of ld, boxes of 128 bytes x
+// `rows` in the 128-byte swizzle; what lies outside reads as zero.
+bool make_load_map(CUtensorMap *m, const void *base, int size, int64_t C, int64_t R, int64_t ld, int rows)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
+    if (!fn)
+        return false;
+    cuuint64_t dims[2] = {(cuuint64_t)C, (cuuint64_t)R};
+    cuuint64_t strides[1] = {(cuuint64_t)(ld * size)};
+    cuuint32_t box[2] = {(cuuint32_t)(128 / size), (cuuint32_t)rows};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(m, size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+              const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int64_t widened_cols(int64_t K) { return (K + 7) / 8 * 8; }
+
+cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *flags, cudaStream_t stream)
+{
+    const int kp = (int)widened_cols(m.K);
+    cudaError_t e = launch_k(k_widen, dim3((unsigned)m.T), dim3(256), 0, stream, true, m.xq, m.ldx, m.K, kp,
+                             static_cast<uint4 *>(workspace));
+    if (e != cudaSuccess)
+        return e;
+    TcArgs a{};
+    a.xs = m.xs;
+    a.ws = m.ws;
+    a.out = m.out;
+    a.flags = flags;
+    a.ldo = m.ldo;
+    a.T = (int)m.T;
+    a.V = (int)m.V;
+    a.K = m.K;
+    a.obf16 = obf16;
+    a.wait_ns = kDefaultWaitNs;
+    // as few token blocks as there can be, all of one width
+    a.ntb = (int)((m.T + kTcMaxN - 1) / kTcMaxN);
+    a.N = (int)(((m.T + a.ntb - 1) / a.ntb + 31) / 32 * 32);
+    a.slots = (512 - 2 * a.N) / kTcSlotCols;
+    if (a.slots > kTcMaxSlots)
+        a.slots = kTcMaxSlots;
+    const size_t stage = kTcWBytes + (size_t)a.N * 128, fixed = 1024 + sizeof(TcTail);
+    a.stages = (int)((kTcSmem - fixed) / stage);
+    if (a.stages > kTcMaxStages)
+        a.stages = kTcMaxStages;
+    a.idesc = 1u << 4 | (uint32_t)(a.N >> 3) << 17 | (uint32_t)(2 * kTcRows >> 4) << 24;  // f32 += f16 f16, K-major
+    CUtensorMap tm_w, tm_x;
+    if (!make_load_map(&tm_w, m.wq, 1, m.K, m.V, m.ldw, kTcRows) ||
+        !make_load_map(&tm_x, workspace, 2, kp, m.T, kp, a.N / 2))
+        return cudaErrorInvalidValue;
+    e = cudaFuncSetAttribute(k_mm_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTcSmem);
+    if (e != cudaSuccess)
+        return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kTcThreads);
+    cfg.dynamicSmemBytes = fixed + (size_t)a.stages * stage;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    const int64_t tiles = (m.V + 2 * kTcRows - 1) / (2 * kTcRows) * a.ntb;
+    cfg.gridDim = dim3(kSms);
+    int fit = 0;
+    e = cudaOccupancyMaxActiveClusters(&fit, k_mm_tc, &cfg);
+    if (e != cudaSuccess)
+        return e;
+    if (fit < 1)
+        return cudaErrorInvalidConfiguration;
+    cfg.gridDim = dim3((unsigned)(2 * (tiles < fit ? tiles : fit)));
+    return cudaLaunchKernelEx(&cfg, k_mm_tc, tm_w, tm_x, a);
+}
+
+template <int TN>
+cudaError_t launch_few(const MmArgs &a, int obf16, int kpad, cudaStream_t stream)
+{
+    const cudaError_t e = cudaFuncSetAttribute(k_mm_few<TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
+    if (e != cudaSuccess)
+        return e;
+    const int64_t ctas = ((a.V + kFewRows - 1) / kFewRows + kFewThreads / 32 - 1) / (kFewThreads / 32);
+    return launch_k(k_mm_few<TN>, dim3((unsigned)(ctas < 2 * kSms ? ctas : 2 * kSms)), dim3(kFewThreads),
+                    (size_t)TN * kpad, stream, true, a, obf16, kpad);
+}
+
+cudaError_t launch_mm(const MmArgs &a, int obf16, void *workspace, unsigned *flags, cudaStream_t stream)
+{
+    if (aligned(a.wq, 16) && a.ldw % 16 == 0) {
+        const int kpad = (a.K + 511) / 512 * 512;
+        if (a.T == 1 && (size_t)kpad <= kFewSmem)
+            return launch_few<1>(a, obf16, kpad, stream);
+        if (a.T == 2 && (size_t)2 * kpad <= kFewSmem)
+            return launch_few<2>(a, obf16, kpad, stream);
+        if (a.T <= 4 && (size_t)4 * kpad <= kFewSmem)
+            return launch_few<4>(a, obf16, kpad, stream);
+        if (a.T <= kFewTokens && (size_t)kFewTokens * kpad <= kFewSmem)
+            return launch_few<kFewTokens>(a, obf16, kpad, stream);
+        return launch_tc(a, obf16, workspace, flags, stream);
+    }
+    const int64_t vb = (a.V + kGV - 1) / kGV, tb = (a.T + kGT - 1) / kGT;
+    return launch_k(k_mm_any, dim3((unsigned)(vb * tb)), dim3(256), 0, stream, true, a, obf16, (unsigned)vb);
+}
+
 }  // namespace
 }  // namespace ember
 
@@ -87,9 +728,9 @@ extern "C" {
 
 size_t ember_matmul_quant_workspace_bytes(int64_t T, int64_t V, int64_t K)
 {
-    if (T < 0 || V < 1 || K < 1 || T > INT32_MAX || V > INT32_MAX || K > kMaxRowCols)
+    if (T < 0 || V < 1 || K < 1 || T > kMaxMmRows || V > kMaxMmRows || K > kMaxRowCols)
         return 0;
-    return 256;
+    return (size_t)(T * widened_cols(K)) * 2 + 256;  // the tokens in fp16
 }
 
 ember_status ember_matmul_quant(const int8_t *xq, int64_t ldx, const float *xs, const int8_t *wq, int64_t ldw,
@@ -102,7 +743,7 @@ ember_status ember_matmul_quant(const int8_t *xq, int64_t ldx, const float *xs, 
         return EMBER_ERR_INVALID_ARG;
     if (!dtype_ok(otype))
         return EMBER_ERR_DTYPE;
-    if (T > INT32_MAX || V > INT32_MAX || K > kMaxRowCols || ldx > (int64_t(1) << 31) || ldw > (int64_t(1) << 31) ||
+    if (T > kMaxMmRows || V > kMaxMmRows || K > kMaxRowCols || ldx > (int64_t(1) << 31) || ldw > (int64_t(1) << 31) ||
         ldo > (int64_t(1) << 32))
         return EMBER_ERR_UNSUPPORTED;
     if (!aligned(xs, 4) || !aligned(ws, 4) || !aligned(out, elem_size(otype)) || !aligned(status, 4) ||
@@ -112,12 +753,11 @@ ember_status ember_matmul_quant(const int8_t *xq, int64_t ldx, const float *xs, 
         return EMBER_OK;
     if (!workspace || bytes < ember_matmul_quant_workspace_bytes(T, V, K))
         return EMBER_ERR_WORKSPACE;
-    MmArgs a{xq, wq, xs, ws, out, ldx, ldw, ldo, T, V, (int)K};
-    const int64_t vb = (V + kGV - 1) / kGV, tb = (T + kGT - 1) / kGT;
-    if (vb * tb > INT32_MAX)
+    // 2^31 tiles of the smallest size are 1.4e14 logits: more than the GPU holds
+    if ((V + kGV - 1) / kGV * ((T + kGT - 1) / kGT) > INT32_MAX)
         return EMBER_ERR_UNSUPPORTED;
-    return launched(launch_k(k_mm_any, dim3((unsigned)(vb * tb)), dim3(256), 0, (cudaStream_t)stream, true, a,
-                             (int)(otype == EMBER_BF16), (unsigned)vb));
+    const MmArgs a{xq, wq, xs, ws, out, ldx, ldw, ldo, T, V, (int)K};
+    return launched(launch_mm(a, otype == EMBER_BF16, workspace, status, (cudaStream_t)stream));
 }
 
 }  // extern "C"

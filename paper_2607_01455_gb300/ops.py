@@ -41,7 +41,7 @@ class _Refused(EmberError, ValueError):
 class Ops:
     """The operators' workspace and sticky status word on one device, for use
     on one stream (calls on different streams share the workspace: give each
-    stream its own object)."""
+    stream its own object).  Before a graph capture, make each call once."""
 
     def __init__(self, device="cuda"):
         dev = torch.device(device)
@@ -50,6 +50,7 @@ class Ops:
         self.device = torch.device("cuda", torch.cuda.current_device() if dev.index is None else dev.index)
         self._lib = lib()
         self._status = self._workspace = None  # made by the first call that needs them, on its stream
+        self._kept = []
 
     # ---- arguments ----
 
@@ -84,9 +85,12 @@ class Ops:
     def _scratch(self, nbytes):
         w = self._workspace
         if w is None or w.numel() < nbytes:
-            if w is not None:
-                w.record_stream(torch.cuda.current_stream(self.device))  # calls in flight still use it
-            w = self._workspace = torch.empty(max(nbytes, 1 << 16), dtype=torch.uint8, device=self.device)
+            # a larger one, at least twice the size; the old one stays for the
+            # calls in flight and the captured graphs that use it
+            size = max(nbytes, 1 << 16) if w is None else max(nbytes, 2 * w.numel())
+            w = torch.empty(size, dtype=torch.uint8, device=self.device)
+            self._kept.append(w)
+            self._workspace = w
         return w
 
     def _status_word(self):
