@@ -6,10 +6,16 @@
 //   loss = sum_t g_t nll_t
 //   dz_tv = g_t (exp(z_tv - lse_t) - [v = y_t])
 //
-// The statistics are a running maximum and a running sum in 32 bits: a thread
-// keeps its own maximum and the sum of exp(z - maximum), and pairs (m, s),
-// (m', s') join as (M, s e^(m-M) + s' e^(m'-M)), M = max(m, m').
+// The statistics are a maximum and a sum in 32 bits: a thread keeps its own
+// maximum and the sum of exp(z - maximum), and pairs (m, s), (m', s') join as
+// (M, s e^(m-M) + s' e^(m'-M)), M = max(m, m').
+//
+// The pass is bound by HBM: each logit read once, each gradient written once.
+// A row of up to 262144 logits is spread over a cluster of up to 8 CTAs and
+// stays in their registers between the statistics and the gradient; the CTAs
+// exchange one pair each through distributed shared memory.
 #include "ember_rows.cuh"
+#include "ember_tc.cuh"
 
 namespace ember {
 namespace {
@@ -182,10 +188,222 @@ __global__ void __launch_bounds__(1024) k_loss_stream(LossArgs a)
     }
 }
 
+// One cluster per row.  The row is cut at the 16-byte groups (32-byte for
+// fp32) of its address into groups of 8 logits, NG per thread; the up to 14
+// logits before the first and after the last whole group go one by one to
+// threads of the first CTA.  The gradient's rows are at the same places of
+// their groups (launch_rows sees to it).
+template <typename ZT, typename DT, bool GRAD, int NG, int MAXT, int MINB>
+__global__ void __launch_bounds__(MAXT, MINB) k_loss_cluster(LossArgs a, int count_here)
+{
+    __shared__ MaxSum part[32];
+    __shared__ MaxSum all[8];
+    __shared__ int nvalid[32];
+    const unsigned C = tc::cluster_count_in(), rank = tc::cluster_rank();
+    const int64_t t = blockIdx.x / C;
+    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5, nwarps = nt >> 5;
+    if (C > 1)
+        tc::cluster_arrive();  // waited for before the first store into another CTA: by then all have started
+    dev::grid_dep_wait();
+    dev::grid_dep_launch();
+
+    const int64_t y = target_of(a, t);
+    const bool on = counts(a, y);
+    const ZT *z = static_cast<const ZT *>(a.z) + t * a.ldz;
+    DT *d = static_cast<DT *>(a.d) + t * a.ldd;
+    const int V = (int)a.V;
+    int head = (int)((8 - ((uintptr_t)z / sizeof(ZT)) % 8) % 8);
+    head = head < V ? head : V;
+    const int ngroups = (V - head) / 8;
+    const int tail = V - head - ngroups * 8;
+    const int first = (int)rank * nt + tid, step = (int)C * nt;
+    // the logit outside the groups that this thread has, or -1
+    int single = -1;
+    if (rank == 0 && tid < head + tail)
+        single = tid < head ? tid : V - tail + (tid - head);
+
+    Raw<ZT, 8> r[NG];
+    float zs = -kInf;
+    if (on) {
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+            const int g = first + k * step;
+            if (g < ngroups)
+                r[k] = load_raw<ZT, 8>(z + head + (int64_t)g * 8);
+        }
+        if (single >= 0) {
+            float f[1];
+            unpack<ZT, 1>(load_raw<ZT, 1>(z + single), f);
+            zs = f[0];
+        }
+    }
+    float zy[1] = {0.f};
+    if (on && rank == 0 && tid == 0)
+        unpack<ZT, 1>(load_raw<ZT, 1>(z + y), zy);
+    // the number of counted tokens: from the kernel before, or, when the
+    // tokens are few, from their targets at once
+    float n = 1.f;
+    if (count_here) {
+        int c = 0;
+        bool bad = false;
+        for (int64_t q = tid; q < a.T; q += nt) {
+            const int64_t yq = target_of(a, q);
+            c += counts(a, yq);
+            bad |= yq != a.ignore && !counts(a, yq);
+        }
+        if (bad && blockIdx.x == 0)
+            atomicOr(a.status, kFlagIdRange);
+        c = __reduce_add_sync(0xffffffffu, c);
+        if (lane == 0)
+            nvalid[warp] = c;
+    } else if (a.mean)
+        n = (float)*a.count;
+
+    MaxSum ms{zs, 0.f};
+#pragma unroll
+    for (int k = 0; k < NG; ++k)
+        if (on && first + k * step < ngroups) {
+            float f[8];
+            unpack<ZT, 8>(r[k], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                ms.m = fmaxf(ms.m, f[e]);
+        }
+    {
+        const float m = finite_max(ms.m);
+        ms.s = exp_of(zs - m);
+#pragma unroll
+        for (int k = 0; k < NG; ++k)
+            if (on && first + k * step < ngroups) {
+                float f[8];
+                unpack<ZT, 8>(r[k], f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    ms.s += exp_of(f[e] - m);
+            }
+    }
+    ms = warp_join(ms);
+    if (lane == 0)
+        part[warp] = ms;
+    __syncthreads();
+    ms = warp_join(lane < nwarps ? part[lane] : MaxSum{-kInf, 0.f});
+    if (C > 1) {
+        // every CTA's pair into every CTA
+        tc::cluster_wait();
+        if (tid < (int)C)
+            tc::store_remote(&all[rank], tid, ms.m, ms.s);
+        tc::cluster_sync();
+        ms = all[0];
+        for (unsigned k = 1; k < C; ++k)
+            ms = join(ms, all[k]);
+    }
+    if (count_here) {
+        int c = 0;
+        for (int k = 0; k < nwarps; ++k)
+            c += nvalid[k];
+        n = (float)c;
+        if (blockIdx.x == 0 && tid == 0)
+            *a.count = c;
+    }
+    const float m = finite_max(ms.m);
+    if (rank == 0 && tid == 0)
+        a.nll[t] = !on ? 0.f : ms.s == 0.f ? kInf : m - zy[0] + logf(ms.s);
+    if constexpr (GRAD) {
+        float g = on ? (a.w ? a.w[t] : 1.f) : 0.f;
+        if (a.mean && on)
+            g /= n;
+        const bool live = on && ms.s != 0.f;
+        const float f = live ? g / ms.s : 0.f;
+        const float hot = live ? g : 0.f;
+        const int yg = on ? ((int)y - head) : -1;  // place of the target among the groups' logits
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+            const int gi = first + k * step;
+            if (gi < ngroups) {
+                float o[8];
+                if (live) {
+                    unpack<ZT, 8>(r[k], o);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        o[e] = exp_of(o[e] - m) * f;
+                    if (yg >= 0 && (yg >> 3) == gi) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if ((yg & 7) == e)
+                                o[e] -= hot;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        o[e] = 0.f;
+                }
+                store_group<DT, 8>(d + head + (int64_t)gi * 8, o);
+            }
+        }
+        if (single >= 0) {
+            const float o[1] = {live ? exp_of(zs - m) * f - (single == (int)y ? hot : 0.f) : 0.f};
+            store_group<DT, 1>(d + single, o);
+        }
+    }
+}
+
+// Threads per CTA and CTAs per row for rows of V logits, or C = 0 where the
+// row does not fit the registers of a cluster.  Four groups a thread (16 KiB
+// of bf16 logits per 256 threads in flight); CTAs of up to 512 threads, so
+// that several rows share an SM and one row's loads cover another's stores.
+struct RowPlan {
+    int C, nt;
+};
+constexpr int kLossGroups = 4;
+constexpr int64_t kCountHere = 512;  // tokens whose targets every CTA counts itself
+
+RowPlan row_plan(int64_t T, int64_t V)
+{
+    RowPlan p{0, 0};
+    const int64_t threads = (V / 8 + kLossGroups - 1) / kLossGroups;
+    int C = 1;
+    while (C < 8 && threads > (int64_t)C * 512)
+        C *= 2;
+    if (threads > (int64_t)C * 1024 || T * C > INT32_MAX)
+        return p;
+    p.C = C;
+    p.nt = (int)((threads + C - 1) / C + 31) / 32 * 32;
+    if (p.nt < 32)
+        p.nt = 32;
+    return p;
+}
+
 template <typename ZT, typename DT, bool GRAD>
 cudaError_t launch_rows(const LossArgs &a, cudaStream_t stream)
 {
-    return launch_k(k_loss_stream<ZT, DT, GRAD>, dim3((unsigned)a.T), dim3(1024), 0, stream, true, a);
+    RowPlan p = row_plan(a.T, a.V);
+    if (GRAD && (((uintptr_t)a.z / sizeof(ZT) - (uintptr_t)a.d / sizeof(DT)) % 8 != 0 || (a.ldz - a.ldd) % 8 != 0))
+        p.C = 0;
+    const bool here = p.C > 0 && a.T <= kCountHere;
+    cudaError_t e = cudaSuccess;
+    if (!here)
+        e = launch_k(k_loss_count, dim3(1), dim3(1024), 0, stream, true, a);
+    if (e != cudaSuccess)
+        return e;
+    if (p.C == 0)
+        return launch_k(k_loss_stream<ZT, DT, GRAD>, dim3((unsigned)a.T), dim3(1024), 0, stream, true, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.T * p.C));
+    cfg.blockDim = dim3(p.nt);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = p.C;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    if (p.nt <= 512)
+        return cudaLaunchKernelEx(&cfg, k_loss_cluster<ZT, DT, GRAD, kLossGroups, 512, sizeof(ZT) == 2 ? 3 : 2>, a,
+                                  (int)here);
+    return cudaLaunchKernelEx(&cfg, k_loss_cluster<ZT, DT, GRAD, kLossGroups, 1024, 1>, a, (int)here);
 }
 
 }  // namespace
@@ -238,16 +456,14 @@ ember_status ember_softmax_loss(const void *logits, int64_t ldz, ember_wdtype zt
     a.mean = mean;
     if (T == 0)
         return launched(cudaMemsetAsync(loss, 0, sizeof(float), s));
-    cudaError_t e = launch_k(k_loss_count, dim3(1), dim3(1024), 0, s, true, a);
-    if (e == cudaSuccess) {
-        const bool zb = ztype == EMBER_BF16, db = dtype == EMBER_BF16;
-        if (!dlogits)
-            e = zb ? launch_rows<bf16_t, bf16_t, false>(a, s) : launch_rows<float, float, false>(a, s);
-        else if (zb)
-            e = db ? launch_rows<bf16_t, bf16_t, true>(a, s) : launch_rows<bf16_t, float, true>(a, s);
-        else
-            e = db ? launch_rows<float, bf16_t, true>(a, s) : launch_rows<float, float, true>(a, s);
-    }
+    const bool zb = ztype == EMBER_BF16, db = dtype == EMBER_BF16;
+    cudaError_t e;
+    if (!dlogits)
+        e = zb ? launch_rows<bf16_t, bf16_t, false>(a, s) : launch_rows<float, float, false>(a, s);
+    else if (zb)
+        e = db ? launch_rows<bf16_t, bf16_t, true>(a, s) : launch_rows<bf16_t, float, true>(a, s);
+    else
+        e = db ? launch_rows<float, bf16_t, true>(a, s) : launch_rows<float, float, true>(a, s);
     if (e == cudaSuccess)
         e = launch_k(k_loss_total, dim3(1), dim3(1024), 0, s, true, a);
     return launched(e);

@@ -139,11 +139,22 @@ __device__ __forceinline__ uint32_t cluster_count()
     asm volatile("mov.u32 %0, %%nclusterid.x;" : "=r"(r));
     return r;
 }
+// CTAs in this cluster.
+__device__ __forceinline__ uint32_t cluster_count_in()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
+    return r;
+}
 // Every thread of every CTA of the cluster: arrive, then wait for all.
 __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+
+// The two halves of a cluster barrier that orders nothing.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 
 // Address of the same shared-memory variable in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t mapa_rank(uint32_t addr, uint32_t rank)
@@ -151,6 +162,13 @@ __device__ __forceinline__ uint32_t mapa_rank(uint32_t addr, uint32_t rank)
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
+}
+
+// Two floats into the variable at `p`'s place in CTA `rank` of the cluster.
+__device__ __forceinline__ void store_remote(void *p, uint32_t rank, float x, float y)
+{
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(mapa_rank(smem_addr(p), rank)), "f"(x), "f"(y)
+                 : "memory");
 }
 
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)

@@ -27,6 +27,8 @@ import torch
 from .ember import (EMBER_BF16, EMBER_ERR_DTYPE, EMBER_ERR_INVALID_ARG, EMBER_F32, EMBER_I32, EMBER_I64, EMBER_OK,
                     EmberError, _check, _current_stream, lib)
 
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
 _TYPES = {torch.bfloat16: EMBER_BF16, torch.float32: EMBER_F32}
 _IDS = {torch.int32: EMBER_I32, torch.int64: EMBER_I64}
 
@@ -48,32 +50,37 @@ class Ops:
         if dev.type != "cuda":
             raise _Refused("Ops", f"a CUDA device is needed, not {dev}")
         self.device = torch.device("cuda", torch.cuda.current_device() if dev.index is None else dev.index)
+        self._index = self.device.index
         self._lib = lib()
         self._status = self._workspace = None  # made by the first call that needs them, on its stream
         self._kept = []
 
     # ---- arguments ----
 
-    def _matrix(self, where, name, t, types=None, shape=None):
+    def _matrix(self, where, name, t, types, shape=None):
         """(address, row stride) of a 2-D tensor with unit stride along its rows."""
-        if t.device != self.device:
-            raise _Refused(where, f"{name} is on {t.device}, not on {self.device}")
-        if types is not None and t.dtype not in types:
-            raise _Refused(where, f"{name} has type {t.dtype}", EMBER_ERR_DTYPE)
-        if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
-            raise _Refused(where, f"{name} has shape {tuple(t.shape)}" + (f", not {shape}" if shape else ", not 2-D"))
-        rows, cols = t.shape
-        sr, sc = t.stride()
-        if cols < 1 or (sc != 1 and cols > 1) or (rows > 1 and sr < cols):
-            raise _Refused(where, f"{name} has strides {t.stride()}: unit stride along rows that do not overlap is needed")
-        return t.data_ptr(), sr if rows > 1 and sr >= cols else cols
-
-    def _vector(self, where, name, t, n, types):
+        size, stride = t.shape, t.stride()
+        if (len(size) == 2 and stride[1] == 1 and stride[0] >= size[1] > 0 and t.get_device() == self._index
+                and t.dtype in types and (shape is None or size == shape)):
+            return t.data_ptr(), stride[0]
         if t.device != self.device:
             raise _Refused(where, f"{name} is on {t.device}, not on {self.device}")
         if t.dtype not in types:
             raise _Refused(where, f"{name} has type {t.dtype}", EMBER_ERR_DTYPE)
-        if t.dim() != 1 or t.numel() != n or (n > 1 and t.stride(0) != 1):
+        if len(size) != 2 or (shape is not None and size != shape):
+            raise _Refused(where, f"{name} has shape {tuple(size)}, not {'two dimensions' if shape is None else tuple(shape)}")
+        # the stride of a single row, and that along a single column, mean nothing
+        if size[1] < 1 or (stride[1] != 1 and size[1] > 1) or (stride[0] < size[1] and size[0] > 1):
+            raise _Refused(where, f"{name} has shape {tuple(size)} and strides {stride}: unit stride along rows that "
+                                  "do not overlap is needed")
+        return t.data_ptr(), max(stride[0], size[1])
+
+    def _vector(self, where, name, t, n, types):
+        if t.get_device() != self._index:
+            raise _Refused(where, f"{name} is on {t.device}, not on {self.device}")
+        if t.dtype not in types:
+            raise _Refused(where, f"{name} has type {t.dtype}", EMBER_ERR_DTYPE)
+        if t.dim() != 1 or t.numel() != n or not t.is_contiguous():
             raise _Refused(where, f"{name} has shape {tuple(t.shape)} and strides {t.stride()}, not {n} in a row")
         return t.data_ptr()
 
@@ -106,6 +113,16 @@ class Ops:
 
     # ---- the norm ----
 
+    def _new(self, shape, dtype):
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _result(self, where, t, shape, dtype, name="out"):
+        """(tensor, address, row stride) of an output: `t`, or a new one without it."""
+        if t is None:
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+            return t, t.data_ptr(), shape[1]
+        return t, *self._matrix(where, name, t, (dtype,), shape)
+
     def rmsnorm(self, x, gain, residual=None, eps=1e-6, out=None, residual_out=None, stream=None):
         """(y, h): y = gain s / sqrt(mean s^2 + eps) over the rows of s = x +
         residual, in x's type, and h = s in the residual's type (None without
@@ -115,24 +132,24 @@ class Ops:
                 return self.rmsnorm(x, gain, residual, eps, out, residual_out)
         w = "rmsnorm"
         px, ldx = self._matrix(w, "x", x, _TYPES)
-        T, D = x.shape
+        shape, xt = x.shape, x.dtype
+        T, D = shape
         pg, gt = self._gain(w, gain, D)
-        pr, ldr, rt, ph, ldh, h = self._residual(w, residual, residual_out, T, D)
-        y = torch.empty((T, D), dtype=x.dtype, device=self.device) if out is None else out
-        py, ldy = self._matrix(w, "out", y, (x.dtype,), (T, D))
-        _check(self._lib.ember_rmsnorm(px, ldx, _TYPES[x.dtype], pr, ldr, rt, pg, gt, T, D, eps, ph, ldh, py, ldy,
-                                       _current_stream()), w)
+        pr, ldr, rt, ph, ldh, h = self._residual(w, residual, residual_out, shape)
+        y, py, ldy = self._result(w, out, shape, xt)
+        _check(self._lib.ember_rmsnorm(px, ldx, _TYPES[xt], pr, ldr, rt, pg, gt, T, D, eps, ph, ldh, py, ldy,
+                                       _raw_stream(self._index)), w)
         return y, h
 
-    def _residual(self, where, residual, residual_out, T, D):
+    def _residual(self, where, residual, residual_out, shape):
         if residual is None:
             if residual_out is not None:
                 raise _Refused(where, "residual_out without a residual")
             return None, 0, EMBER_F32, None, 0, None
-        pr, ldr = self._matrix(where, "residual", residual, _TYPES, (T, D))
-        h = torch.empty((T, D), dtype=residual.dtype, device=self.device) if residual_out is None else residual_out
-        ph, ldh = self._matrix(where, "residual_out", h, (residual.dtype,), (T, D))
-        return pr, ldr, _TYPES[residual.dtype], ph, ldh, h
+        pr, ldr = self._matrix(where, "residual", residual, _TYPES, shape)
+        rt = residual.dtype
+        h, ph, ldh = self._result(where, residual_out, shape, rt, "residual_out")
+        return pr, ldr, _TYPES[rt], ph, ldh, h
 
     def rmsnorm_quant(self, x, gain, residual=None, eps=1e-6, residual_out=None, stream=None):
         """(q, scales, h): the norm in 8 bits, y about q * scales[:, None]."""
@@ -143,17 +160,17 @@ class Ops:
         px, ldx = self._matrix(w, "x", x, _TYPES)
         T, D = x.shape
         pg, gt = self._gain(w, gain, D)
-        pr, ldr, rt, ph, ldh, h = self._residual(w, residual, residual_out, T, D)
+        pr, ldr, rt, ph, ldh, h = self._residual(w, residual, residual_out, x.shape)
         q, ldq, scales = self._rows8(T, D)
         _check(self._lib.ember_rmsnorm_quant(px, ldx, _TYPES[x.dtype], pr, ldr, rt, pg, gt, T, D, eps, ph, ldh,
-                                             q.data_ptr(), ldq, scales.data_ptr(), _current_stream()), w)
+                                             q.data_ptr(), ldq, scales.data_ptr(), _raw_stream(self._index)), w)
         return q, scales, h
 
     def _rows8(self, T, D):
         """New 8-bit rows, each on a 16-byte boundary, and their scales."""
         ld = (D + 15) // 16 * 16
-        q = torch.empty((T, ld), dtype=torch.int8, device=self.device)
-        return q if ld == D else q[:, :D], ld, torch.empty(T, dtype=torch.float32, device=self.device)
+        q = self._new((T, ld), torch.int8)
+        return q if ld == D else q[:, :D], ld, self._new(T, torch.float32)
 
     def rmsnorm_backward(self, dy, h, gain, eps=1e-6, dres=None, out=None, stream=None):
         """(dx, dgain) of the norm at h; dres, what reaches h past the norm, is
@@ -163,17 +180,16 @@ class Ops:
                 return self.rmsnorm_backward(dy, h, gain, eps, dres, out)
         w = "rmsnorm_backward"
         ph, ldh = self._matrix(w, "h", h, _TYPES)
-        T, D = h.shape
-        same = (h.dtype,)
-        py, ldy = self._matrix(w, "dy", dy, same, (T, D))
-        pr, ldr = (None, 0) if dres is None else self._matrix(w, "dres", dres, same, (T, D))
+        shape, same = h.shape, (h.dtype,)
+        T, D = shape
+        py, ldy = self._matrix(w, "dy", dy, same, shape)
+        pr, ldr = (None, 0) if dres is None else self._matrix(w, "dres", dres, same, shape)
         pg, gt = self._gain(w, gain, D)
-        dx = torch.empty((T, D), dtype=h.dtype, device=self.device) if out is None else out
-        pd, ldd = self._matrix(w, "out", dx, same, (T, D))
-        dgain = torch.empty(D, dtype=torch.float32, device=self.device)
+        dx, pd, ldd = self._result(w, out, shape, h.dtype)
+        dgain = self._new(D, torch.float32)
         ws = self._scratch(self._lib.ember_rmsnorm_backward_workspace_bytes(T, D))
         _check(self._lib.ember_rmsnorm_backward(py, ldy, ph, ldh, pr, ldr, _TYPES[h.dtype], pg, gt, T, D, eps, pd, ldd,
-                                                dgain.data_ptr(), ws.data_ptr(), ws.numel(), _current_stream()), w)
+                                                dgain.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(self._index)), w)
         return dx, dgain
 
     # ---- 8 bits ----
@@ -189,7 +205,7 @@ class Ops:
         T, D = x.shape
         q, ldq, scales = self._rows8(T, D)
         _check(self._lib.ember_quantize_rows(px, ldx, _TYPES[x.dtype], T, D, q.data_ptr(), ldq, scales.data_ptr(),
-                                             _current_stream()), w)
+                                             _raw_stream(self._index)), w)
         return q, scales
 
     def dequantize_rows(self, q, scales, dtype=torch.bfloat16, out=None, stream=None):
@@ -203,9 +219,8 @@ class Ops:
         ps = self._vector(w, "scales", scales, T, (torch.float32,))
         if dtype not in _TYPES:
             raise _Refused(w, f"an output of type {dtype}", EMBER_ERR_DTYPE)
-        y = torch.empty((T, D), dtype=dtype, device=self.device) if out is None else out
-        py, ldy = self._matrix(w, "out", y, (dtype,), (T, D))
-        _check(self._lib.ember_dequantize_rows(pq, ldq, ps, T, D, py, ldy, _TYPES[dtype], _current_stream()), w)
+        y, py, ldy = self._result(w, out, q.shape, dtype)
+        _check(self._lib.ember_dequantize_rows(pq, ldq, ps, T, D, py, ldy, _TYPES[dtype], _raw_stream(self._index)), w)
         return y
 
     def matmul_quant(self, xq, xs, wq, ws, dtype=torch.bfloat16, out=None, stream=None):
@@ -225,12 +240,11 @@ class Ops:
         pws = self._vector(w, "ws", ws, V, (torch.float32,))
         if dtype not in _TYPES:
             raise _Refused(w, f"an output of type {dtype}", EMBER_ERR_DTYPE)
-        o = torch.empty((T, V), dtype=dtype, device=self.device) if out is None else out
-        po, ldo = self._matrix(w, "out", o, (dtype,), (T, V))
+        o, po, ldo = self._result(w, out, (T, V), dtype)
         work = self._scratch(self._lib.ember_matmul_quant_workspace_bytes(T, V, K))
         _check(self._lib.ember_matmul_quant(px, ldx, pxs, pw, ldw, pws, T, V, K, po, ldo, _TYPES[dtype],
                                             work.data_ptr(), work.numel(), self._status_word(),
-                                            _current_stream()), w)
+                                            _raw_stream(self._index)), w)
         return o
 
     # ---- the loss ----
@@ -260,41 +274,45 @@ class Ops:
             # rows of the gradient start where those of the logits do in a group
             # of 16 bytes, so that both take wide accesses
             ld = ldz if ldz < V + 64 else (V + 7) // 8 * 8
-            d = torch.empty_strided((T, V), (ld, 1), dtype=dt, device=self.device) if out is None else out
-            pd, ldd = self._matrix(w, "out", d, (dt,), (T, V))
-        loss = torch.empty((), dtype=torch.float32, device=self.device)
-        nll = torch.empty(T, dtype=torch.float32, device=self.device)
+            if out is None:
+                d = torch.empty_strided((T, V), (ld, 1), dtype=dt, device=self.device)
+                pd, ldd = d.data_ptr(), ld
+            else:
+                d = out
+                pd, ldd = self._matrix(w, "out", d, (dt,), logits.shape)
+        loss = self._new((), torch.float32)
+        nll = self._new(T, torch.float32)
         work = self._scratch(self._lib.ember_softmax_loss_workspace_bytes(T))
         _check(self._lib.ember_softmax_loss(pz, ldz, _TYPES[logits.dtype], py, _IDS[targets.dtype], pw, ignore_index,
                                             int(reduction == "mean"), T, V, loss.data_ptr(), nll.data_ptr(), pd, ldd,
                                             _TYPES[dt], work.data_ptr(), work.numel(), self._status_word(),
-                                            _current_stream()), w)
+                                            _raw_stream(self._index)), w)
         return loss, nll, d
 
     # ---- gradients ----
 
     def _list(self, where, tensors, out):
         """The host arrays of a call over many tensors: addresses, sizes, types."""
-        dev = self.device
         for t in tensors:
-            if t.device != dev or not t.is_contiguous():
+            if t.get_device() != self._index or not t.is_contiguous():
                 raise _Refused(where, f"a gradient of shape {tuple(t.shape)}, strides {t.stride()} on {t.device}: "
-                                      f"contiguous tensors on {dev} are needed")
+                                      f"contiguous tensors on {self.device} are needed")
+        kinds = [t.dtype for t in tensors]
         try:
-            types = array("i", [_TYPES[t.dtype] for t in tensors])
+            types = array("i", [_TYPES[d] for d in kinds])
         except KeyError as e:
             raise _Refused(where, f"a gradient of type {e.args[0]}", EMBER_ERR_DTYPE) from None
         numel = array("q", [t.numel() for t in tensors])
         ptrs = array("Q", [t.data_ptr() for t in tensors])
-        outs = ptrs
-        if out is not None:
-            if len(out) != len(tensors):
-                raise _Refused(where, f"{len(out)} outputs for {len(tensors)} gradients")
-            for t, o in zip(tensors, out):
-                if o.dtype != t.dtype or o.shape != t.shape or o.device != dev or not o.is_contiguous():
-                    raise _Refused(where, f"an output of shape {tuple(o.shape)}, type {o.dtype} for a gradient of "
-                                          f"shape {tuple(t.shape)}, type {t.dtype}")
-            outs = array("Q", [o.data_ptr() for o in out])
+        if out is None:
+            return ptrs, ptrs, numel, types
+        if len(out) != len(tensors):
+            raise _Refused(where, f"{len(out)} outputs for {len(tensors)} gradients")
+        for t, o, d in zip(tensors, out, kinds):
+            if o.shape != t.shape or o.dtype != d or o.get_device() != self._index or not o.is_contiguous():
+                raise _Refused(where, f"an output of shape {tuple(o.shape)}, type {o.dtype} for a gradient of "
+                                      f"shape {tuple(t.shape)}, type {t.dtype}")
+        outs = array("Q", [o.data_ptr() for o in out])
         return ptrs, outs, numel, types
 
     def grad_norm(self, tensors, stream=None):
@@ -305,11 +323,11 @@ class Ops:
         w = "grad_norm"
         tensors = list(tensors)
         ptrs, _, numel, types = self._list(w, tensors, None)
-        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        norm = self._new((), torch.float32)
         n = len(tensors)
         work = self._scratch(self._lib.ember_clip_workspace_bytes(n))
         _check(self._lib.ember_grad_norm(n, ptrs.buffer_info()[0], numel.buffer_info()[0], types.buffer_info()[0],
-                                         norm.data_ptr(), work.data_ptr(), work.numel(), _current_stream()), w)
+                                         norm.data_ptr(), work.data_ptr(), work.numel(), _raw_stream(self._index)), w)
         return norm
 
     def clip_grads(self, tensors, max_norm, out=None, eps=1e-6, stream=None):
@@ -322,12 +340,12 @@ class Ops:
         w = "clip_grads"
         tensors = list(tensors)
         ptrs, outs, numel, types = self._list(w, tensors, out)
-        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        norm = self._new((), torch.float32)
         n = len(tensors)
         work = self._scratch(self._lib.ember_clip_workspace_bytes(n))
         _check(self._lib.ember_clip_grads(n, ptrs.buffer_info()[0], outs.buffer_info()[0], numel.buffer_info()[0],
                                           types.buffer_info()[0], max_norm, eps, norm.data_ptr(), work.data_ptr(),
-                                          work.numel(), _current_stream()), w)
+                                          work.numel(), _raw_stream(self._index)), w)
         return norm
 
     def device_status(self, stream=None):

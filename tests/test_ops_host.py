@@ -119,18 +119,18 @@ def test_the_python_layer_names_what_it_refuses():
     with pytest.raises(E.EmberError, match="CUDA device"):
         Ops("cpu")
     o = Ops.__new__(Ops)  # the checks themselves touch no GPU
-    o.device = torch.device("cpu")
+    o.device, o._index = torch.device("cpu"), -1  # what a CPU tensor's get_device() gives
     z = torch.zeros(4, 8)
     assert o._matrix("f", "x", z, (torch.float32,))[1] == 8
-    assert o._matrix("f", "x", z[:, 2:5])[1] == 8
+    assert o._matrix("f", "x", z[:, 2:5], (torch.float32,))[1] == 8
     for bad in (z.T, z[:, ::2], z[0], z[:1].expand(4, 8), z[:, :0]):
         with pytest.raises(ValueError, match="x has"):
-            o._matrix("f", "x", bad)
+            o._matrix("f", "x", bad, (torch.float32,))
     with pytest.raises(E.EmberError) as ex:
         o._matrix("f", "x", z, (torch.bfloat16,))
     assert ex.value.status == DTYPE
     with pytest.raises(ValueError, match="shape"):
-        o._matrix("f", "x", z, None, (8, 4))
+        o._matrix("f", "x", z, (torch.float32,), (8, 4))
     with pytest.raises(ValueError, match="not 3 in a row"):
         o._vector("f", "w", z[0], 3, (torch.float32,))
     with pytest.raises(ValueError, match="contiguous"):
