@@ -25,9 +25,41 @@ using namespace rows;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInf = __builtin_huge_valf();
 
-// 2^x, and e^x of a difference: the difference is exact where it matters
-// (near zero), so its rounding costs a relative 2^-23 |x| at most.
-__device__ __forceinline__ float exp_of(float d) { return exp2f(d * kLog2e); }
+// 2^x within two ulps, results below 2^-126 as zero: they are less than one
+// rounding of the row's sum, which is at least 1.
+__device__ __forceinline__ float exp2_of(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// e^d of a difference: it is exact where it matters (near zero), so the
+// rounding of d log2(e) costs a relative 2^-23 |d| at most.
+__device__ __forceinline__ float exp_of(float d) { return exp2_of(d * kLog2e); }
+
+// Pairs of floats in one instruction.
+struct f2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ f2 make2(float x, float y)
+{
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void split2(f2 a, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a.v)); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b)
+{
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b)
+{
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
 
 struct MaxSum {
     float m, s;
@@ -35,20 +67,20 @@ struct MaxSum {
 // A maximum of -inf (nothing seen but -inf) is replaced by 0 in differences,
 // so that exp gives 0 and not NaN.
 __device__ __forceinline__ float finite_max(float m) { return m == -kInf ? 0.f : m; }
-__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b)
+// The pairs of the lanes that differ in the bits below WIDTH (a power of two),
+// joined: the maximum first, so that every sum is rescaled once.
+template <int WIDTH>
+__device__ __forceinline__ MaxSum lanes_join(MaxSum v)
 {
-    MaxSum r;
-    r.m = fmaxf(a.m, b.m);
-    const float m = finite_max(r.m);
-    r.s = a.s * exp_of(a.m - m) + b.s * exp_of(b.m - m);
-    return r;
-}
-__device__ __forceinline__ MaxSum warp_join(MaxSum v)
-{
+    float m = v.m;
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1)
-        v = join(v, {__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.s, o)});
-    return v;
+    for (int o = WIDTH / 2; o >= 1; o >>= 1)
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float s = v.s * exp_of(v.m - finite_max(m));
+#pragma unroll
+    for (int o = WIDTH / 2; o >= 1; o >>= 1)
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+    return {m, s};
 }
 
 struct LossArgs {
@@ -165,11 +197,11 @@ __global__ void __launch_bounds__(1024) k_loss_stream(LossArgs a)
         ms.m = m;
         ms.s += exp_of(f[0] - finite_max(m));
     }
-    ms = warp_join(ms);
+    ms = lanes_join<32>(ms);
     if ((threadIdx.x & 31) == 0)
         part[threadIdx.x >> 5] = ms;
     __syncthreads();
-    ms = warp_join(part[threadIdx.x & 31]);
+    ms = lanes_join<32>(part[threadIdx.x & 31]);
     const float m = finite_max(ms.m);
     if (threadIdx.x == 0)
         a.nll[t] = ms.s == 0.f ? kInf : m - zy[0] + logf(ms.s);
@@ -188,58 +220,136 @@ __global__ void __launch_bounds__(1024) k_loss_stream(LossArgs a)
     }
 }
 
-// One cluster per row.  The row is cut at the 16-byte groups (32-byte for
-// fp32) of its address into groups of 8 logits, NG per thread; the up to 14
-// logits before the first and after the last whole group go one by one to
-// threads of the first CTA.  The gradient's rows are at the same places of
-// their groups (launch_rows sees to it).
-template <typename ZT, typename DT, bool GRAD, int NG, int MAXT, int MINB>
-__global__ void __launch_bounds__(MAXT, MINB) k_loss_cluster(LossArgs a, int count_here)
+// Rows in the registers of a cluster.  Cluster q of n takes rows q, q + n,
+// ...  A row is cut at the 16-byte units of its address (8 bf16 or 4 fp32
+// logits); CTA `rank` has a contiguous slice of the units, which one bulk copy
+// brings to its shared memory.  A thread takes up to 64 logits from there,
+// finds their maximum and keeps e^(z - maximum) in registers: one exponential
+// per logit, since the gradient is a multiple of it.  The buffer is then free:
+// the copy of the cluster's next row runs while this one is reduced, exchanged
+// and stored.  The CTAs exchange their pairs by asynchronous stores that
+// complete on the receiver's mbarrier; a cluster barrier would wait, row by
+// row, until the gradients stored before it had left the SM.  The logits
+// before the first and after the last whole unit go one by one to threads of
+// the first CTA.  The gradient's rows are at the same places of their units
+// (launch_rows sees to it).
+//
+// A wait that gives up sets the timeout flag; from then on the CTA starts no
+// copy and waits for nothing, and runs its rows to their end, still sending
+// its pairs.
+template <typename T, int N>
+__device__ __forceinline__ void unpack_unit(const uint4 &r, float (&f)[N])
 {
+    const unsigned u[4] = {r.x, r.y, r.z, r.w};
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            f[2 * k] = dev::bf16_lo(u[k]);
+            f[2 * k + 1] = dev::bf16_hi(u[k]);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            f[k] = __uint_as_float(u[k]);
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_unit(T *p, const float (&f)[N])
+{
+    if constexpr (N == 8)
+        store_group<T, 8>(p, f);
+    else if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+    else
+        *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+}
+
+// Where the whole units of row t lie, and the slice of this CTA.
+template <typename ZT>
+struct Cut {
+    static constexpr int VE = 16 / sizeof(ZT);
+    int head, tail, units, per, u0, n;  // logits before and after the units; units per CTA; this CTA's units
+    __device__ __forceinline__ Cut(const ZT *z, int V, int log_C, int rank)
+    {
+        head = (int)((VE - ((uintptr_t)z / sizeof(ZT)) % VE) % VE);
+        head = head < V ? head : V;
+        units = (V - head) / VE;
+        tail = V - head - units * VE;
+        per = (units + (1 << log_C) - 1) >> log_C;
+        u0 = rank * per;
+        n = units - u0 < per ? units - u0 : per;
+        n = n > 0 ? n : 0;
+    }
+};
+
+// The larger of two units, value by value (a NaN loses; it is found in the sum).
+template <typename ZT>
+__device__ __forceinline__ float unit_max(const uint4 &r)
+{
+    if constexpr (sizeof(ZT) == 2) {
+        auto h = [](unsigned u) { return *reinterpret_cast<const __nv_bfloat162 *>(&u); };
+        const __nv_bfloat162 m = __hmax2(__hmax2(h(r.x), h(r.y)), __hmax2(h(r.z), h(r.w)));
+        return fmaxf(__low2float(m), __high2float(m));
+    } else
+        return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)),
+                     fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+}
+
+constexpr int kPerThread = 64;  // logits of a row per thread
+constexpr int kRowThreads = 256;  // two CTAs per SM; rows too long for them take twice as many, one CTA per SM
+
+template <typename ZT, typename DT, bool GRAD, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT > kRowThreads ? 1 : 2) k_loss_rows(LossArgs a, int count_here)
+{
+    constexpr int VE = Cut<ZT>::VE;
+    constexpr int NU = kPerThread / VE;
+    extern __shared__ __align__(128) unsigned char buf[];  // this CTA's slice of a row
     __shared__ MaxSum part[32];
-    __shared__ MaxSum all[8];
+    __shared__ __align__(8) MaxSum all[2][8];
     __shared__ int nvalid[32];
-    const unsigned C = tc::cluster_count_in(), rank = tc::cluster_rank();
-    const int64_t t = blockIdx.x / C;
+    __shared__ uint64_t full, joined[2];
+    __shared__ int abort_;
+    const int C = (int)tc::cluster_count_in(), rank = (int)tc::cluster_rank();
+    const int log_C = __ffs(C) - 1;
+    const int64_t first = blockIdx.x / C, step = gridDim.x / C;
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5, nwarps = nt >> 5;
+    const int V = (int)a.V;
+    const ZT *zbase = static_cast<const ZT *>(a.z);
+    const uint32_t bar = tc::smem_addr(&full);
+    volatile int *abort = &abort_;
+    if (tid == 0) {
+        tc::mbar_init(bar, 1);
+        tc::mbar_init(tc::smem_addr(&joined[0]), 1);
+        tc::mbar_init(tc::smem_addr(&joined[1]), 1);
+        abort_ = 0;
+        for (int k = 0; k < 16; ++k)  // the places of CTAs that the cluster does not have stay so
+            all[k >> 3][k & 7] = {-kInf, 0.f};
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     if (C > 1)
-        tc::cluster_arrive();  // waited for before the first store into another CTA: by then all have started
+        tc::cluster_arrive_release();  // waited for before the first store into another CTA: by then all are ready
     dev::grid_dep_wait();
     dev::grid_dep_launch();
 
-    const int64_t y = target_of(a, t);
-    const bool on = counts(a, y);
-    const ZT *z = static_cast<const ZT *>(a.z) + t * a.ldz;
-    DT *d = static_cast<DT *>(a.d) + t * a.ldd;
-    const int V = (int)a.V;
-    int head = (int)((8 - ((uintptr_t)z / sizeof(ZT)) % 8) % 8);
-    head = head < V ? head : V;
-    const int ngroups = (V - head) / 8;
-    const int tail = V - head - ngroups * 8;
-    const int first = (int)rank * nt + tid, step = (int)C * nt;
-    // the logit outside the groups that this thread has, or -1
-    int single = -1;
-    if (rank == 0 && tid < head + tail)
-        single = tid < head ? tid : V - tail + (tid - head);
-
-    Raw<ZT, 8> r[NG];
-    float zs = -kInf;
-    if (on) {
-#pragma unroll
-        for (int k = 0; k < NG; ++k) {
-            const int g = first + k * step;
-            if (g < ngroups)
-                r[k] = load_raw<ZT, 8>(z + head + (int64_t)g * 8);
+    // The copy of row t's slice, by thread 0; rows that do not count need none.
+    auto start = [&](int64_t t, int64_t y) {
+        const ZT *z = zbase + t * a.ldz;
+        const Cut<ZT> q(z, V, log_C, rank);
+        if (!counts(a, y) || q.n == 0)
+            return;
+        tc::mbar_expect_tx(bar, (uint32_t)q.n * 16);
+        tc::bulk_load(tc::smem_addr(buf), z + q.head + (int64_t)q.u0 * VE, (uint32_t)q.n * 16, bar);
+    };
+    auto wait = [&](uint32_t b, uint32_t parity) {
+        if (!*abort && !tc::mbar_wait(b, parity, abort, kDefaultWaitNs)) {
+            atomicOr(a.status, kFlagTimeout);
+            *abort = 1;
         }
-        if (single >= 0) {
-            float f[1];
-            unpack<ZT, 1>(load_raw<ZT, 1>(z + single), f);
-            zs = f[0];
-        }
-    }
-    float zy[1] = {0.f};
-    if (on && rank == 0 && tid == 0)
-        unpack<ZT, 1>(load_raw<ZT, 1>(z + y), zy);
+    };
+    int64_t y = target_of(a, first);
+    int64_t ynext = first + step < a.T ? target_of(a, first + step) : 0;  // read a row ahead of its use
+    if (tid == 0)
+        start(first, y);
     // the number of counted tokens: from the kernel before, or, when the
     // tokens are few, from their targets at once
     float n = 1.f;
@@ -256,128 +366,227 @@ __global__ void __launch_bounds__(MAXT, MINB) k_loss_cluster(LossArgs a, int cou
         c = __reduce_add_sync(0xffffffffu, c);
         if (lane == 0)
             nvalid[warp] = c;
-    } else if (a.mean)
-        n = (float)*a.count;
-
-    MaxSum ms{zs, 0.f};
-#pragma unroll
-    for (int k = 0; k < NG; ++k)
-        if (on && first + k * step < ngroups) {
-            float f[8];
-            unpack<ZT, 8>(r[k], f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                ms.m = fmaxf(ms.m, f[e]);
-        }
-    {
-        const float m = finite_max(ms.m);
-        ms.s = exp_of(zs - m);
-#pragma unroll
-        for (int k = 0; k < NG; ++k)
-            if (on && first + k * step < ngroups) {
-                float f[8];
-                unpack<ZT, 8>(r[k], f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    ms.s += exp_of(f[e] - m);
-            }
-    }
-    ms = warp_join(ms);
-    if (lane == 0)
-        part[warp] = ms;
-    __syncthreads();
-    ms = warp_join(lane < nwarps ? part[lane] : MaxSum{-kInf, 0.f});
-    if (C > 1) {
-        // every CTA's pair into every CTA
-        tc::cluster_wait();
-        if (tid < (int)C)
-            tc::store_remote(&all[rank], tid, ms.m, ms.s);
-        tc::cluster_sync();
-        ms = all[0];
-        for (unsigned k = 1; k < C; ++k)
-            ms = join(ms, all[k]);
-    }
-    if (count_here) {
-        int c = 0;
+        __syncthreads();
+        c = 0;
         for (int k = 0; k < nwarps; ++k)
             c += nvalid[k];
         n = (float)c;
         if (blockIdx.x == 0 && tid == 0)
             *a.count = c;
+    } else {
+        if (a.mean)
+            n = (float)*a.count;
+        __syncthreads();  // the mbarriers are initialised
     }
-    const float m = finite_max(ms.m);
-    if (rank == 0 && tid == 0)
-        a.nll[t] = !on ? 0.f : ms.s == 0.f ? kInf : m - zy[0] + logf(ms.s);
-    if constexpr (GRAD) {
-        float g = on ? (a.w ? a.w[t] : 1.f) : 0.f;
-        if (a.mean && on)
-            g /= n;
-        const bool live = on && ms.s != 0.f;
-        const float f = live ? g / ms.s : 0.f;
-        const float hot = live ? g : 0.f;
-        const int yg = on ? ((int)y - head) : -1;  // place of the target among the groups' logits
+
+    const float inv_n = a.mean ? 1.f / n : 1.f;  // infinite when no token counts, but then no row uses it
+    // rows a whole number of units apart are all cut alike
+    const bool alike = a.ldz % VE == 0;
+    Cut<ZT> c(zbase, V, log_C, rank);
+    uint32_t parity = 0;
+    uint32_t round = 0;  // row number of this cluster: the exchange alternates between two buffers
+    for (int64_t t = first; t < a.T; t += step, ++round) {
+        const ZT *z = zbase + t * a.ldz;
+        DT *d = static_cast<DT *>(a.d) + t * a.ldd;
+        if (!alike)
+            c = Cut<ZT>(z, V, log_C, rank);
+        const bool on = counts(a, y);
+        const bool more = t + step < a.T;
+        const int64_t yafter = t + 2 * step < a.T ? target_of(a, t + 2 * step) : 0;
+        const float w = a.w && on ? a.w[t] : 1.f;
+        // the logit outside the units that this thread has, or -1
+        int single = -1;
+        if (rank == 0 && tid < c.head + c.tail)
+            single = tid < c.head ? tid : V - c.tail + (tid - c.head);
+        float zs = -kInf;
+        if (on && single >= 0) {
+            float f[1];
+            unpack<ZT, 1>(load_raw<ZT, 1>(z + single), f);
+            zs = f[0];
+        }
+        const int have = on ? c.n : 0;  // units in the buffer
+        uint4 r[NU];
+        if (have > 0) {
+            wait(bar, parity);
+            parity ^= 1u;
+        }
 #pragma unroll
-        for (int k = 0; k < NG; ++k) {
-            const int gi = first + k * step;
-            if (gi < ngroups) {
-                float o[8];
-                if (live) {
-                    unpack<ZT, 8>(r[k], o);
+        for (int k = 0; k < NU; ++k) {
+            // what is behind the slice counts as masked out
+            constexpr unsigned fill = sizeof(ZT) == 2 ? 0xFF80FF80u : 0xFF800000u;
+            if ((k + 1) * nt <= have)
+                r[k] = reinterpret_cast<const uint4 *>(buf)[tid + k * nt];
+            else
+                r[k] = tid + k * nt < have ? reinterpret_cast<const uint4 *>(buf)[tid + k * nt]
+                                           : make_uint4(fill, fill, fill, fill);
+        }
+        __syncthreads();
+        if (tid == 0 && more && !*abort)
+            start(t + step, ynext);
+
+        float mt = zs;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        o[e] = exp_of(o[e] - m) * f;
-                    if (yg >= 0 && (yg >> 3) == gi) {
+        for (int k = 0; k < NU; ++k)
+            mt = fmaxf(mt, unit_max<ZT>(r[k]));
+        const float m0 = finite_max(mt);
+        float e[NU][VE];  // e^(z - m0)
+        const float es = exp_of(zs - m0);
+        f2 sum = make2(es, 0.f), sum2 = make2(0.f, 0.f);
+        const f2 minus = make2(-m0, -m0), scale = make2(kLog2e, kLog2e);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if ((yg & 7) == e)
-                                o[e] -= hot;
-                    }
-                } else {
+        for (int k = 0; k < NU; ++k) {
+            unpack_unit<ZT, VE>(r[k], e[k]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        o[e] = 0.f;
-                }
-                store_group<DT, 8>(d + head + (int64_t)gi * 8, o);
+            for (int q = 0; q < VE; q += 2) {
+                const f2 x = mul2(add2(make2(e[k][q], e[k][q + 1]), minus), scale);
+                split2(x, e[k][q], e[k][q + 1]);
+                e[k][q] = exp2_of(e[k][q]);
+                e[k][q + 1] = exp2_of(e[k][q + 1]);
+                f2 &to = q & 2 ? sum2 : sum;
+                to = add2(to, make2(e[k][q], e[k][q + 1]));
             }
         }
-        if (single >= 0) {
-            const float o[1] = {live ? exp_of(zs - m) * f - (single == (int)y ? hot : 0.f) : 0.f};
-            store_group<DT, 1>(d + single, o);
+        MaxSum ms;
+        ms.m = mt;
+        {
+            float x, y2;
+            split2(add2(sum, sum2), x, y2);
+            ms.s = x + y2;
         }
+        ms = lanes_join<32>(ms);
+        if (nwarps > 1) {
+            if (lane == 0)
+                part[warp] = ms;
+            __syncthreads();
+            ms = lanes_join<32>(lane < nwarps ? part[lane] : MaxSum{-kInf, 0.f});
+        }
+        if (C > 1) {
+            if (round == 0)
+                tc::cluster_wait();
+            // every CTA's pair into every CTA
+            const uint32_t p = round & 1u;
+            const uint32_t jb = tc::smem_addr(&joined[p]);
+            if (tid == 0)
+                tc::mbar_expect_tx(jb, (uint32_t)C * sizeof(MaxSum));
+            if (tid < C)
+                tc::store_remote_async(&all[p][rank], tid, ms.m, ms.s, jb);
+            wait(jb, round >> 1 & 1u);
+            ms = lanes_join<8>(all[p][lane & 7]);
+        }
+        const float m = finite_max(ms.m);
+        const bool live = on && ms.s != 0.f;
+        if (!on && rank == 0 && tid == 0)
+            a.nll[t] = 0.f;
+        const float g = w * inv_n;
+        const float gs = __fdividef(g, ms.s);  // a sum is between 1 and 2^18: within two ulps
+        const float f = live ? exp_of(m0 - m) * gs : 0.f;
+        // the target, by the thread that has it among its logits
+        const int yu = on ? (int)y - c.head - c.u0 * VE : -1;  // its place among this slice's logits
+        const bool mine = yu >= 0 && yu < c.n * VE && yu / VE % nt == tid;
+        float hot = 0.f;  // its gradient
+        if (mine) {
+            // read again from the row: the copy's buffer may hold the next one already
+            float zy[1];
+            unpack<ZT, 1>(load_raw<ZT, 1>(z + y), zy);
+            a.nll[t] = live ? (m - zy[0]) + logf(ms.s) : kInf;
+            hot = live ? exp_of(zy[0] - m) * gs - g : 0.f;
+        }
+        if (single >= 0 && on && single == (int)y)
+            a.nll[t] = live ? (m - zs) + logf(ms.s) : kInf;
+        if constexpr (GRAD) {
+            // a row that does not count, or is -inf throughout, has only zeros in e
+            const f2 ff = make2(f, f);
+#pragma unroll
+            for (int k = 0; k < NU; ++k) {
+                const int u = tid + k * nt;
+#pragma unroll
+                for (int q = 0; q < VE; q += 2)
+                    split2(mul2(make2(e[k][q], e[k][q + 1]), ff), e[k][q], e[k][q + 1]);
+                if (u < c.n)
+                    store_unit<DT, VE>(d + c.head + (int64_t)(c.u0 + u) * VE, e[k]);
+            }
+            if (mine) {
+                const float o[1] = {hot};
+                store_group<DT, 1>(d + y, o);
+            }
+            if (single >= 0) {
+                const float o[1] = {live ? es * f - (single == (int)y ? g : 0.f) : 0.f};
+                store_group<DT, 1>(d + single, o);
+            }
+        }
+        y = ynext;
+        ynext = yafter;
     }
+    if (tid == 0 && *abort)
+        tc::mbar_wait_final(bar, parity ^ 1u);  // the copy that was given up has left this CTA's shared memory
 }
 
-// Threads per CTA and CTAs per row for rows of V logits, or C = 0 where the
-// row does not fit the registers of a cluster.  Four groups a thread (16 KiB
-// of bf16 logits per 256 threads in flight); CTAs of up to 512 threads, so
-// that several rows share an SM and one row's loads cover another's stores.
+// Threads per CTA and CTAs per row for rows of V logits; C = 0 where a row
+// does not fit the registers of a cluster.
 struct RowPlan {
     int C, nt;
+    size_t smem;
 };
-constexpr int kLossGroups = 4;
 constexpr int64_t kCountHere = 512;  // tokens whose targets every CTA counts itself
 
-RowPlan row_plan(int64_t T, int64_t V)
+RowPlan row_plan(int64_t T, int64_t V, int esize)
 {
-    RowPlan p{0, 0};
-    const int64_t threads = (V / 8 + kLossGroups - 1) / kLossGroups;
+    RowPlan p{0, 0, 0};
+    const int64_t units = V / (16 / esize) + 1, nu = kPerThread / (16 / esize);
     int C = 1;
-    while (C < 8 && threads > (int64_t)C * 512)
+    while (C < 8 && units > C * kRowThreads * nu)
         C *= 2;
-    if (threads > (int64_t)C * 1024 || T * C > INT32_MAX)
+    const int64_t per = (units + C - 1) / C;
+    if (per > 2 * kRowThreads * nu || T * C > INT32_MAX)
         return p;
     p.C = C;
-    p.nt = (int)((threads + C - 1) / C + 31) / 32 * 32;
-    if (p.nt < 32)
-        p.nt = 32;
+    p.nt = (int)((per + nu - 1) / nu + 31) / 32 * 32;
+    p.smem = (size_t)per * 16;
     return p;
+}
+
+// As many clusters as run at once, each with a share of the rows; one per row
+// when there are few.
+template <typename K>
+cudaError_t launch_cluster(K kernel, const LossArgs &a, const RowPlan &p, bool here, cudaStream_t stream)
+{
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10);
+    if (e != cudaSuccess)
+        return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.T * p.C));
+    cfg.blockDim = dim3(p.nt);
+    cfg.dynamicSmemBytes = p.smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = p.C;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    if (a.T * p.C > kSms) {
+        cfg.numAttrs = 1;
+        int fit = 0;
+        e = cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg);
+        if (e != cudaSuccess)
+            return e;
+        if (fit < 1)
+            return cudaErrorInvalidConfiguration;
+        if (a.T > fit)
+            cfg.gridDim = dim3((unsigned)fit * p.C);
+    }
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a, (int)here);
 }
 
 template <typename ZT, typename DT, bool GRAD>
 cudaError_t launch_rows(const LossArgs &a, cudaStream_t stream)
 {
-    RowPlan p = row_plan(a.T, a.V);
-    if (GRAD && (((uintptr_t)a.z / sizeof(ZT) - (uintptr_t)a.d / sizeof(DT)) % 8 != 0 || (a.ldz - a.ldd) % 8 != 0))
+    RowPlan p = row_plan(a.T, a.V, sizeof(ZT));
+    constexpr int VE = 16 / sizeof(ZT);
+    if (GRAD && (((uintptr_t)a.z / sizeof(ZT) - (uintptr_t)a.d / sizeof(DT)) % VE != 0 || (a.ldz - a.ldd) % VE != 0))
         p.C = 0;
     const bool here = p.C > 0 && a.T <= kCountHere;
     cudaError_t e = cudaSuccess;
@@ -387,23 +596,9 @@ cudaError_t launch_rows(const LossArgs &a, cudaStream_t stream)
         return e;
     if (p.C == 0)
         return launch_k(k_loss_stream<ZT, DT, GRAD>, dim3((unsigned)a.T), dim3(1024), 0, stream, true, a);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.T * p.C));
-    cfg.blockDim = dim3(p.nt);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = p.C;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    if (p.nt <= 512)
-        return cudaLaunchKernelEx(&cfg, k_loss_cluster<ZT, DT, GRAD, kLossGroups, 512, sizeof(ZT) == 2 ? 3 : 2>, a,
-                                  (int)here);
-    return cudaLaunchKernelEx(&cfg, k_loss_cluster<ZT, DT, GRAD, kLossGroups, 1024, 1>, a, (int)here);
+    if (p.nt <= kRowThreads)
+        return launch_cluster(k_loss_rows<ZT, DT, GRAD, kRowThreads>, a, p, here, stream);
+    return launch_cluster(k_loss_rows<ZT, DT, GRAD, 2 * kRowThreads>, a, p, here, stream);
 }
 
 }  // namespace

@@ -152,9 +152,12 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// The two halves of a cluster barrier that orders nothing.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+// The two halves of a cluster barrier.
+__device__ __forceinline__ void cluster_arrive_release()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // Address of the same shared-memory variable in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t mapa_rank(uint32_t addr, uint32_t rank)
@@ -164,16 +167,28 @@ __device__ __forceinline__ uint32_t mapa_rank(uint32_t addr, uint32_t rank)
     return r;
 }
 
-// Two floats into the variable at `p`'s place in CTA `rank` of the cluster.
-__device__ __forceinline__ void store_remote(void *p, uint32_t rank, float x, float y)
+// Two floats, asynchronously, into the variable at `p`'s place in CTA `rank`
+// of the cluster; their 8 bytes complete on the mbarrier at bar's place there.
+__device__ __forceinline__ void store_remote_async(void *p, uint32_t rank, float x, float y, uint32_t bar)
 {
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(mapa_rank(smem_addr(p), rank)), "f"(x), "f"(y)
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(
+                     mapa_rank(smem_addr(p), rank)),
+                 "f"(x), "f"(y), "r"(mapa_rank(bar, rank))
                  : "memory");
 }
 
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+// `bytes` (a multiple of 16) from global memory into this CTA's shared
+// memory, both on 16-byte boundaries; they complete on `bar`.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
 }
 
 // One box of the tensor map into this CTA's shared memory; its bytes complete on the
