@@ -61,27 +61,18 @@ __device__ __forceinline__ int tensor_of(const TensorList<CAP> &l, unsigned c)
     return lo;
 }
 
-// Sum of squares of N values in 64 bits, exact beyond 32 bits' range.
+// Sum of squares of N values: in 32 bits, in four chains, or nothing and
+// `wide` set where it must be done in 64.  Zeros need no more.
 template <int N>
-__device__ __noinline__ double squares64(const float (&v)[N])
-{
-    double s = 0.0;
-    for (int e = 0; e < N; ++e)
-        if (v[e] != 0.f)
-            s += (double)v[e] * (double)v[e];
-    return s;
-}
-template <int N>
-__device__ __forceinline__ double squares(const float (&v)[N])
+__device__ __forceinline__ double squares(const float (&v)[N], bool &wide)
 {
     float p[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < N; ++e)
         p[e & 3] = fmaf(v[e], v[e], p[e & 3]);
     const float s = (p[0] + p[1]) + (p[2] + p[3]);
-    if (s >= 1e-25f && s <= 1e30f)
-        return (double)s;
-    return squares64<N>(v);
+    wide = !(s >= 1e-25f && s <= 1e30f);
+    return wide ? 0.0 : (double)s;
 }
 
 // Elements of a tensor before its first 16-byte (bf16) or 32-byte (fp32)
@@ -94,6 +85,25 @@ __device__ __forceinline__ int head_of(const T *p, int64_t n)
     return h < n ? h : (int)n;
 }
 
+// This thread's groups of a chunk.  A chunk that lies inside the tensor loads
+// without a test between the loads, so that all of them are in flight.
+template <typename T, int NG>
+__device__ __forceinline__ void load_chunk(const T *body, int64_t g0, int64_t ngroups, Raw<T, 8> (&r)[NG])
+{
+    if (g0 + NG * kClipThreads <= ngroups) {
+        const T *p = body + (g0 + threadIdx.x) * 8;
+#pragma unroll
+        for (int k = 0; k < NG; ++k)
+            r[k] = load_raw<T, 8>(p + k * (kClipThreads * 8));
+    } else {
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+            const int64_t g = g0 + k * kClipThreads + threadIdx.x;
+            r[k] = g < ngroups ? load_raw<T, 8>(body + g * 8) : zero_raw<T, 8>();
+        }
+    }
+}
+
 template <typename T, int NG>
 __device__ __forceinline__ double chunk_squares(const T *p, int64_t n, unsigned chunk)
 {
@@ -102,11 +112,7 @@ __device__ __forceinline__ double chunk_squares(const T *p, int64_t n, unsigned 
     const int64_t g0 = (int64_t)chunk * (NG * kClipThreads);
     const T *body = p + head;
     Raw<T, 8> r[NG];
-#pragma unroll
-    for (int k = 0; k < NG; ++k) {
-        const int64_t g = g0 + k * kClipThreads + threadIdx.x;
-        r[k] = g < ngroups ? load_raw<T, 8>(body + g * 8) : zero_raw<T, 8>();
-    }
+    load_chunk<T, NG>(body, g0, ngroups, r);
     float v[NG * 8];
 #pragma unroll
     for (int k = 0; k < NG; ++k) {
@@ -116,7 +122,18 @@ __device__ __forceinline__ double chunk_squares(const T *p, int64_t n, unsigned 
         for (int e = 0; e < 8; ++e)
             v[k * 8 + e] = f[e];
     }
-    double s = squares<NG * 8>(v);
+    bool wide;
+    double s = squares<NG * 8>(v, wide);
+    if (wide)  // read again: it is rare, and the values need not be kept for it
+        for (int k = 0; k < NG; ++k) {
+            const int64_t g = g0 + k * kClipThreads + threadIdx.x;
+            for (int e = 0; g < ngroups && e < 8; ++e) {
+                float f[1];
+                unpack<T, 1>(load_raw<T, 1>(body + g * 8 + e), f);
+                if (f[0] != 0.f)
+                    s += (double)f[0] * (double)f[0];
+            }
+        }
     if (chunk == 0) {  // the elements outside whole groups, at most 14
         const int tail = (int)(n - head - ngroups * 8);
         if ((int)threadIdx.x < head + tail) {
@@ -191,13 +208,8 @@ __device__ __forceinline__ void chunk_scale(const T *p, T *o, int64_t n, unsigne
     const int64_t g0 = (int64_t)chunk * (NG * kClipThreads);
     const T *body = p + head;
     Raw<T, 8> r[NG];
-#pragma unroll
-    for (int k = 0; k < NG; ++k) {
-        const int64_t g = g0 + k * kClipThreads + threadIdx.x;
-        if (g < ngroups)
-            r[k] = load_raw<T, 8>(body + g * 8);
-    }
-    const bool whole = (uintptr_t)(o + head) % 16 == 0;
+    load_chunk<T, NG>(body, g0, ngroups, r);
+    const bool whole = (uintptr_t)(o + head) % (8 * sizeof(T)) == 0;
 #pragma unroll
     for (int k = 0; k < NG; ++k) {
         const int64_t g = g0 + k * kClipThreads + threadIdx.x;

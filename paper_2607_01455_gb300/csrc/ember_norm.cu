@@ -369,6 +369,142 @@ __global__ void __launch_bounds__(MAXT) k_rmsnorm_back(BackArgs a)
     }
 }
 
+// The same for long rows of whole groups, one row per CTA at a time.  The rows
+// of dy, h and dres come through a ring of two rows in shared memory, filled by
+// asynchronous copies; a thread copies what it will read itself, so the ring
+// needs no barrier, and the next two rows are on their way while one is
+// reduced and written.
+constexpr int kBackStages = 2;
+
+__device__ __forceinline__ void copy16(void *smem, const void *p)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p)
+                 : "memory");
+}
+
+template <typename XT, bool RES, int MAXT, int MINB>
+__global__ void __launch_bounds__(MAXT, MINB) k_rmsnorm_back_ring(BackArgs a)
+{
+    constexpr int NV = 4;                   // groups of 8 per thread
+    constexpr int GB = 8 * sizeof(XT);      // bytes of a group
+    constexpr int NIN = RES ? 3 : 2;
+    extern __shared__ __align__(128) unsigned char ring[];  // [stage][input][group of the row]
+    __shared__ float part[2][2][32];
+    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, w = tid >> 5, nw = nt >> 5;
+    const int groups = a.D / 8;
+    const int row_bytes = a.D * (int)sizeof(XT);
+    dev::grid_dep_wait();
+    dev::grid_dep_launch();
+
+    auto fetch = [&](int64_t row, int stage) {
+        if (row < a.T) {
+            const unsigned char *in[3] = {
+                reinterpret_cast<const unsigned char *>(static_cast<const XT *>(a.dy) + row * a.lddy),
+                reinterpret_cast<const unsigned char *>(static_cast<const XT *>(a.h) + row * a.ldh),
+                RES ? reinterpret_cast<const unsigned char *>(static_cast<const XT *>(a.dres) + row * a.lddres)
+                    : nullptr};
+#pragma unroll
+            for (int i = 0; i < NIN; ++i) {
+                unsigned char *to = ring + (size_t)(stage * NIN + i) * row_bytes;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    const int g = k * nt + tid;
+                    if (g < groups) {
+#pragma unroll
+                        for (int b = 0; b < GB; b += 16)
+                            copy16(to + g * GB + b, in[i] + g * GB + b);
+                    }
+                }
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto held = [&](int stage, int i, int g) {
+        const unsigned char *p = ring + (size_t)(stage * NIN + i) * row_bytes + g * GB;
+        Raw<XT, 8> r;
+        if constexpr (sizeof(XT) == 2)
+            r.v = *reinterpret_cast<const uint4 *>(p);
+        else {
+            r.a = reinterpret_cast<const float4 *>(p)[0];
+            r.b = reinterpret_cast<const float4 *>(p)[1];
+        }
+        return r;
+    };
+
+    float acc[NV][8];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            acc[k][e] = 0.f;
+    const float inv_D = 1.f / (float)a.D;
+#pragma unroll
+    for (int s = 0; s < kBackStages; ++s)
+        fetch(blockIdx.x + (int64_t)s * gridDim.x, s);
+    int stage = 0, par = 0;
+    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, par ^= 1) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kBackStages - 1) : "memory");
+        float ss = 0.f, dot = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int g = k * nt + tid;
+            if (g < groups) {
+                float ga[8], fy[8], fh[8];
+                load_gain<8>(a.gain, a.gbf16, g * 8, ga);
+                unpack<XT, 8>(held(stage, 0, g), fy);
+                unpack<XT, 8>(held(stage, 1, g), fh);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    ss = fmaf(fh[e], fh[e], ss);
+                    dot = fmaf(fy[e] * ga[e], fh[e], dot);
+                }
+            }
+        }
+        ss = warp_sum(ss);
+        dot = warp_sum(dot);
+        if (nw > 1) {
+            if (lane == 0) {
+                part[par][0][w] = ss;
+                part[par][1][w] = dot;
+            }
+            __syncthreads();
+            ss = warp_sum(lane < nw ? part[par][0][lane] : 0.f);
+            dot = warp_sum(lane < nw ? part[par][1][lane] : 0.f);
+        }
+        const float r = 1.f / sqrtf(ss * inv_D + a.eps);
+        const float c = r * r * (dot * inv_D);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int g = k * nt + tid;
+            if (g < groups) {
+                float ga[8], fy[8], fh[8], o[8];
+                load_gain<8>(a.gain, a.gbf16, g * 8, ga);
+                unpack<XT, 8>(held(stage, 0, g), fy);
+                unpack<XT, 8>(held(stage, 1, g), fh);
+                if constexpr (RES)
+                    unpack<XT, 8>(held(stage, 2, g), o);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = r * fmaf(-fh[e], c, fy[e] * ga[e]);
+                    o[e] = RES ? v + o[e] : v;
+                    acc[k][e] = fmaf(fy[e], fh[e] * r, acc[k][e]);
+                }
+                store_group<XT, 8>(static_cast<XT *>(a.dx) + row * a.lddx + g * 8, o);
+            }
+        }
+        fetch(row + (int64_t)kBackStages * gridDim.x, stage);
+        stage = stage + 1 == kBackStages ? 0 : stage + 1;
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    float *p = a.partial + (int64_t)blockIdx.x * a.D;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int g = k * nt + tid;
+        if (g < groups)
+            store_group<float, 8>(p + g * 8, acc[k]);
+    }
+}
+
 // dgain_j = the sum of the n partial rows of column j: 32 columns a CTA, each
 // by 32 threads that take every 32nd row, then joined in order.
 __global__ void __launch_bounds__(1024) k_dgain(const float *__restrict__ partial, int n, int D,
@@ -392,20 +528,34 @@ __global__ void __launch_bounds__(1024) k_dgain(const float *__restrict__ partia
 
 struct BackPlan {
     int vec, nv, tpr, block, grid;
+    bool ring;
+    size_t smem;
     int64_t parts;  // partial rows
 };
 
-// Two CTAs of 512 threads (or their like) per SM.
-BackPlan back_plan(int64_t T, int64_t D, bool grouped8)
+// Long rows of whole groups go through the ring: from 1024 columns on (a warp
+// of four groups a thread; shorter rows share a CTA), as long as two rows of
+// three inputs fit the shared memory.  The rest keeps one row in registers.
+BackPlan back_plan(int64_t T, int64_t D, int esize, bool grouped8)
 {
-    BackPlan p;
+    BackPlan p{};
+    const size_t smem = (size_t)kBackStages * 3 * D * esize;
+    p.ring = grouped8 && D >= 1024 && smem <= 200 << 10;
     p.vec = grouped8 ? 8 : 1;
-    p.nv = grouped8 ? (D <= 2048 ? 1 : D <= 8192 ? 2 : 4) : (D <= 4096 ? 4 : 32);
+    p.nv = p.ring ? 4 : grouped8 ? (D <= 2048 ? 1 : D <= 8192 ? 2 : 4) : (D <= 4096 ? 4 : 32);
     p.tpr = threads_per_row(D, p.vec, p.nv);
-    p.block = p.tpr < kMinBlock ? kMinBlock : p.tpr;
+    p.block = p.ring ? p.tpr : p.tpr < kMinBlock ? kMinBlock : p.tpr;
     const int64_t rpc = p.block / p.tpr;
     const int64_t want = (T + rpc - 1) / rpc;
-    const int64_t most = (int64_t)kSms * (p.block >= 1024 ? 1 : 1024 / p.block);
+    int per_sm = p.block >= 1024 ? 1 : 1024 / p.block;
+    if (p.ring) {
+        p.smem = smem;
+        per_sm = (int)((220 << 10) / (smem + 2048));
+        const int by_regs = 512 / p.block;
+        per_sm = per_sm < by_regs ? per_sm : by_regs;
+        per_sm = per_sm > 8 ? 8 : per_sm < 1 ? 1 : per_sm;
+    }
+    const int64_t most = (int64_t)kSms * per_sm;
     p.grid = (int)(want < most ? want : most);
     p.parts = p.grid * rpc;
     return p;
@@ -415,7 +565,14 @@ template <typename XT, bool RES>
 cudaError_t launch_back(BackArgs a, const BackPlan &p, cudaStream_t stream)
 {
     a.tpr = p.tpr;
-    auto go = [&](auto kernel) { return launch_k(kernel, dim3(p.grid), dim3(p.block), 0, stream, true, a); };
+    auto go = [&](auto kernel) { return launch_k(kernel, dim3(p.grid), dim3(p.block), p.smem, stream, true, a); };
+    if (p.ring) {
+        auto ring = [&](auto kernel) {
+            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10);
+            return e == cudaSuccess ? go(kernel) : e;
+        };
+        return p.block <= 256 ? ring(k_rmsnorm_back_ring<XT, RES, 256, 2>) : ring(k_rmsnorm_back_ring<XT, RES, 512, 1>);
+    }
     if (p.vec == 8) {
         if (p.nv == 1)
             return go(k_rmsnorm_back<XT, RES, 8, 1, 256>);
@@ -502,7 +659,7 @@ ember_status norm_common(NormArgs &a, bool &grouped8, const void *x, int64_t ldx
     a.gbf16 = gtype == EMBER_BF16;
     a.eps = eps;
     grouped8 = D % 8 == 0 && grouped(x, ldx, xtype) && grouped(residual, ldr, rtype) && grouped(h, ldh, rtype) &&
-               aligned(gain, 16);
+               aligned(gain, 8 * elem_size(gtype));
     return EMBER_OK;
 }
 
@@ -601,8 +758,12 @@ size_t ember_rmsnorm_backward_workspace_bytes(int64_t T, int64_t D)
 {
     if (T < 0 || D < 1 || T > INT32_MAX || D > kMaxRowCols)
         return 0;
-    const int64_t a = back_plan(T, D, true).parts, b = back_plan(T, D, false).parts;
-    return sizeof(float) * (size_t)((a > b ? a : b) * D);
+    int64_t most = 0;
+    for (int k = 0; k < 4; ++k) {
+        const int64_t n = back_plan(T, D, k & 1 ? 4 : 2, k >> 1).parts;
+        most = most > n ? most : n;
+    }
+    return sizeof(float) * (size_t)(most * D);
 }
 
 ember_status ember_rmsnorm_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *dres,
@@ -624,8 +785,8 @@ ember_status ember_rmsnorm_backward(const void *dy, int64_t lddy, const void *h,
     if (T == 0)  // no rows: the sums are zero
         return launched(cudaMemsetAsync(dgain, 0, sizeof(float) * (size_t)D, (cudaStream_t)stream));
     const bool grouped8 = D % 8 == 0 && grouped(dy, lddy, type) && grouped(h, ldh, type) &&
-                          grouped(dres, lddres, type) && grouped(dx, lddx, type) && aligned(gain, 16);
-    const BackPlan p = back_plan(T, D, grouped8);
+                          grouped(dres, lddres, type) && grouped(dx, lddx, type) && aligned(gain, 8 * elem_size(gtype));
+    const BackPlan p = back_plan(T, D, (int)elem_size(type), grouped8);
     if (!workspace || bytes < sizeof(float) * (size_t)(p.parts * D))
         return EMBER_ERR_WORKSPACE;
     BackArgs a{};

@@ -13,8 +13,10 @@ constexpr int kMaxRowCols = 32768;  // widest row of the norm operators
 
 struct bf16_t { unsigned short u; };
 
-// A group of VEC elements as it is in memory: 8 (16 bytes of bf16, two times
-// 16 of fp32) or 1.  Kept packed between the load and its uses.
+// A group of VEC elements as it is in memory: 8 (16 bytes of bf16, 32 of fp32,
+// one access each) or 1.  Kept packed between the load and its uses.  The
+// loads are volatile so that a thread's loads are issued together, before the
+// first use; no kernel stores where another thread's later load may read.
 template <typename T, int VEC> struct Raw;
 template <> struct Raw<bf16_t, 8> { uint4 v; };
 template <> struct Raw<bf16_t, 1> { unsigned short v; };
@@ -26,12 +28,16 @@ __device__ __forceinline__ Raw<T, VEC> load_raw(const T *p)
 {
     Raw<T, VEC> r;
     if constexpr (sizeof(T) == 2 && VEC == 8)
-        r.v = *reinterpret_cast<const uint4 *>(p);
+        asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r.v.x), "=r"(r.v.y), "=r"(r.v.z), "=r"(r.v.w)
+                     : "l"(p));
     else if constexpr (sizeof(T) == 2)
         r.v = p->u;
     else if constexpr (VEC == 8) {
-        r.a = reinterpret_cast<const float4 *>(p)[0];
-        r.b = reinterpret_cast<const float4 *>(p)[1];
+        asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(r.a.x), "=f"(r.a.y), "=f"(r.a.z), "=f"(r.a.w), "=f"(r.b.x), "=f"(r.b.y), "=f"(r.b.z),
+                       "=f"(r.b.w)
+                     : "l"(p));
     } else
         r.v = *p;
     return r;
@@ -85,10 +91,11 @@ __device__ __forceinline__ void store_group(T *p, const float (&f)[VEC])
                                                    pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
     else if constexpr (sizeof(T) == 2)
         p->u = dev::f2bf(f[0]);
-    else if constexpr (VEC == 8) {
-        reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-        reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-    } else
+    else if constexpr (VEC == 8)
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]),
+                     "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7])
+                     : "memory");
+    else
         *p = f[0];
 }
 
@@ -134,7 +141,7 @@ inline size_t elem_size(int t) { return t == EMBER_BF16 ? 2 : 4; }
 // Whether every row of a matrix of this type starts on a group of 8 elements.
 inline bool grouped(const void *p, int64_t ld, int dtype)
 {
-    return p == nullptr || (aligned(p, 16) && (ld * (int64_t)elem_size(dtype)) % 16 == 0 && ld % 8 == 0);
+    return p == nullptr || (aligned(p, 8 * elem_size(dtype)) && ld % 8 == 0);
 }
 inline ember_status launched(cudaError_t e)
 {
