@@ -37,30 +37,6 @@ __device__ __forceinline__ float exp2_of(float x)
 // rounding of d log2(e) costs a relative 2^-23 |d| at most.
 __device__ __forceinline__ float exp_of(float d) { return exp2_of(d * kLog2e); }
 
-// Pairs of floats in one instruction.
-struct f2 {
-    unsigned long long v;
-};
-__device__ __forceinline__ f2 make2(float x, float y)
-{
-    f2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ void split2(f2 a, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a.v)); }
-__device__ __forceinline__ f2 add2(f2 a, f2 b)
-{
-    f2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ f2 mul2(f2 a, f2 b)
-{
-    f2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-
 struct MaxSum {
     float m, s;
 };
@@ -341,7 +317,7 @@ __global__ void __launch_bounds__(MAXT, MAXT > kRowThreads ? 1 : 2) k_loss_rows(
         tc::bulk_load(tc::smem_addr(buf), z + q.head + (int64_t)q.u0 * VE, (uint32_t)q.n * 16, bar);
     };
     auto wait = [&](uint32_t b, uint32_t parity) {
-        if (!*abort && !tc::mbar_wait(b, parity, abort, kDefaultWaitNs)) {
+        if (!*abort && !tc::mbar_spin(b, parity, abort, kDefaultWaitNs)) {
             atomicOr(a.status, kFlagTimeout);
             *abort = 1;
         }

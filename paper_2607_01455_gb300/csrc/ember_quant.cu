@@ -225,17 +225,19 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_mm_few(MmArgs a, int obf16, 
 // Per block of 128 along K each CTA
 //   - gets its 128 rows of the table as they are, 16 KiB of 8-bit integers, by
 //     TMA into 128-byte swizzled shared memory;
-//   - widens them to fp16 in registers (a thread per row, 128 values) and
-//     stores them in tensor memory as the A operand, 64 columns: shared memory
-//     sees 8 bits per value of the table, not 8 + 16 + 16;
+//   - widens them to fp16 in registers (a thread per row and half, 64 values)
+//     and stores them in tensor memory as the A operand, in slots of 32
+//     columns: shared memory sees 8 bits per value of the table, not 8 + 16 + 16;
 //   - gets its half of the tokens' block, already fp16 (k_widen writes them
 //     once per call), by TMA.
 // Roles (512 threads per CTA, one CTA per SM, persistent over tiles):
-//   warp 0      issues the TMA loads
+//   warps 0, 2  issue the TMA loads of the table and of the tokens: two rings,
+//               since a block of the table is free again once it is widened,
+//               the tokens' only after their MMAs
 //   warp 1      allocates tensor memory; in the even CTA issues the MMAs
 //   warps 4-7   epilogue: scales and stores an accumulator (two of them, so
 //               that it overlaps the next tile's MMAs)
-//   warps 8-15  widen: two sets of four warps take the blocks in turn
+//   warps 8-15  widen: two sets of four warps, one per half of a block
 // Every wait is bounded; one that gives up sets the timeout flag, stops every
 // role, and the kernel returns after its copies and MMAs in flight are done.
 // ---------------------------------------------------------------------------
@@ -245,22 +247,24 @@ constexpr int kTcRows = 128;        // rows of the table per CTA
 constexpr int kTcK = 128;           // block along K
 constexpr int kTcThreads = 512;
 constexpr int kTcMaxN = 192;        // two accumulators and two A slots fill tensor memory
-constexpr int kTcMaxStages = 8, kTcMaxSlots = 4;
+constexpr int kTcMaxStages = 10, kTcMaxSlots = 8;
 constexpr int kTcWBytes = kTcRows * kTcK;
-constexpr int kTcSlotCols = kTcK / 2;  // fp16 pairs
+constexpr int kTcHalf = kTcK / 2;        // K of a slot of A
+constexpr int kTcSlotCols = kTcHalf / 2;  // fp16 pairs
 constexpr size_t kTcSmem = 227 << 10;
 
 struct TcTail {
     uint64_t wfull[kTcMaxStages];   // each CTA: its rows of the table landed
-    uint64_t wempty[kTcMaxStages];  // each CTA: read by its four widening warps
+    uint64_t wempty[kTcMaxStages];  // each CTA: read by its eight widening warps
     uint64_t bfull[kTcMaxStages];   // even CTA: both halves of the tokens landed
-    uint64_t bempty[kTcMaxStages];  // each CTA: the MMAs of the stage are done
+    uint64_t bempty[kTcMaxStages];  // each CTA: the MMAs of the stage are done (passed on by a widening warp)
     uint64_t afull[kTcMaxSlots];    // even CTA: both CTAs' A slots written
-    uint64_t aempty[kTcMaxSlots];   // each CTA: the MMAs of the slot are done
+    uint64_t aempty[kTcMaxSlots / 2];  // each CTA: the MMAs of a block, a pair of slots, are done
     uint64_t tfull[2], tempty[2];   // accumulators, as in the LM-head kernel
     uint64_t drain;
     uint32_t tmem_base;
     int abort;
+    float xs[4][kTcMaxN];  // the tokens' scales of a tile, a copy per epilogue warp
 };
 
 struct TcArgs {
@@ -269,7 +273,7 @@ struct TcArgs {
     unsigned *flags;
     int64_t ldo;
     int T, V, K;
-    int N, ntb, stages, slots, obf16;
+    int N, ntb, wstages, bstages, slots, obf16;
     uint32_t idesc;
     uint64_t wait_ns;
 };
@@ -339,6 +343,43 @@ __global__ void __launch_bounds__(256) k_widen(const int8_t *__restrict__ xq, in
     }
 }
 
+// One channel's column of an accumulator, scaled, into nt rows of the output.
+// The lanes of a warp hold 32 neighbouring channels: a store per token writes
+// 64 or 128 bytes of a row in one piece.
+__device__ __forceinline__ void put(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put(unsigned short *p, float v) { *p = dev::f2bf(v); }
+template <typename T>
+__device__ __forceinline__ void write_tile(T *p, int64_t ldo, uint32_t d_tmem, const float *xs, float ws, int nt, bool on)
+{
+    const f2 w2 = make2(ws, ws);
+    for (int c = 0; c < nt; c += 32) {
+        float d[32];
+        tmem_load32(d_tmem + c, d);
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(xs + c + e);
+            split2(mul2(mul2(make2(d[e], d[e + 1]), make2(x.x, x.y)), w2), d[e], d[e + 1]);
+            split2(mul2(mul2(make2(d[e + 2], d[e + 3]), make2(x.z, x.w)), w2), d[e + 2], d[e + 3]);
+        }
+        if (on) {
+            if (c + 32 <= nt) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    put(p, d[e]);
+                    p += ldo;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (c + e < nt) {
+                        put(p, d[e]);
+                        p += ldo;
+                    }
+            }
+        }
+    }
+}
+
 __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -351,11 +392,11 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
     unsigned char *smem =
         reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(tc_smem_raw) + 1023) & ~(uintptr_t)1023);
     const int b_box = a.N / 2 * 128;  // N / 2 tokens x 64 fp16
-    const int stage_bytes = kTcWBytes + 2 * b_box;
-    TcTail *tail = reinterpret_cast<TcTail *>(smem + (size_t)a.stages * stage_bytes);
+    unsigned char *bring = smem + (size_t)a.wstages * kTcWBytes;
+    TcTail *tail = reinterpret_cast<TcTail *>(bring + (size_t)a.bstages * 2 * b_box);
     volatile int *abort = &tail->abort;
 
-    const int warp = threadIdx.x >> 5;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);  // uniform, and seen to be
     const int lane = threadIdx.x & 31;
     const int rank = (int)cluster_rank();
     const bool leader = rank == 0;
@@ -364,15 +405,18 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
     const int tile0 = (int)cluster_id(), tstep = (int)cluster_count();
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < a.stages; ++s) {
+        for (int s = 0; s < a.wstages; ++s) {
             mbar_init(smem_addr(&tail->wfull[s]), 1);
-            mbar_init(smem_addr(&tail->wempty[s]), 4);
+            mbar_init(smem_addr(&tail->wempty[s]), 8);
+        }
+        for (int s = 0; s < a.bstages; ++s) {
             mbar_init(smem_addr(&tail->bfull[s]), 1);
             mbar_init(smem_addr(&tail->bempty[s]), 1);
         }
         for (int s = 0; s < a.slots; ++s) {
             mbar_init(smem_addr(&tail->afull[s]), 8);  // four warps in each CTA
-            mbar_init(smem_addr(&tail->aempty[s]), 1);
+            if (s % 2 == 0)
+                mbar_init(smem_addr(&tail->aempty[s / 2]), 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_addr(&tail->tfull[s]), 1);
@@ -395,42 +439,46 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
     __syncthreads();
     cluster_sync();  // no peer may signal this CTA's barriers before they are initialised
     tc_fence_after();
-    const uint32_t tmem = tail->tmem_base;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tail->tmem_base, 0);
     const uint32_t slot0 = tmem + 2 * a.N;
     dev::grid_dep_wait();
     dev::grid_dep_launch();
 
-    if (warp == 0 && lane == 0) {
-        // ---------------- TMA producer (both CTAs) ----------------
+    if ((warp == 0 || warp == 2) && lane == 0) {
+        // ---------------- TMA producers (both CTAs) ----------------
+        const bool tokens = warp == 2;
+        const int stages = tokens ? a.bstages : a.wstages;
+        uint64_t *full = tokens ? tail->bfull : tail->wfull, *empty = tokens ? tail->bempty : tail->wempty;
         int stage = 0;
         uint32_t phase = 0;
         uint32_t issued = 0, parity = 0;  // a bit per stage: a copy was issued, the parity of its last phase
         asm volatile("fence.proxy.async.global;" ::: "memory");  // the tokens were written by plain stores
-        const uint64_t pol_w = l2_policy(a.ntb > 1 ? 0 : 2);  // the table streams when every tile is read once
-        const uint64_t pol_x = l2_policy(1);
+        // the table streams when every block is read once
+        const uint64_t pol = l2_policy(tokens ? 1 : a.ntb > 1 ? 0 : 2);
         bool ok = true;
         for (int tile = tile0; tile < ntiles && ok; tile += tstep) {
             const int vrow = (tile / a.ntb * 2 + rank) * kTcRows;
             const int trow = tile % a.ntb * a.N + rank * (a.N / 2);
             for (int kb = 0; kb < kblocks; ++kb) {
-                if (!mbar_wait(smem_addr(&tail->wempty[stage]), phase ^ 1u, abort, a.wait_ns) ||
-                    !mbar_wait(smem_addr(&tail->bempty[stage]), phase ^ 1u, abort, a.wait_ns)) {
+                if (!mbar_spin(smem_addr(&empty[stage]), phase ^ 1u, abort, a.wait_ns)) {
                     ok = false;
                     break;
                 }
-                const uint32_t wbar = smem_addr(&tail->wfull[stage]);
-                const uint32_t bbar = smem_addr(&tail->bfull[stage]);
-                mbar_expect_tx(wbar, kTcWBytes);
-                if (leader)
-                    mbar_expect_tx(bbar, 4 * b_box);  // both CTAs' halves, two boxes each
+                const uint32_t bar = smem_addr(&full[stage]);
                 issued |= 1u << stage;
                 parity = (parity & ~(1u << stage)) | phase << stage;
-                const uint32_t dst = smem_addr(smem + (size_t)stage * stage_bytes);
-                const uint32_t lead = mapa_rank(bbar, 0);
-                tma_load_2d(dst, &tm_w, kb * kTcK, vrow, wbar, pol_w);
-                tma_load_2d(dst + kTcWBytes, &tm_x, kb * kTcK, trow, lead, pol_x);
-                tma_load_2d(dst + kTcWBytes + b_box, &tm_x, kb * kTcK + 64, trow, lead, pol_x);
-                if (++stage == a.stages) {
+                if (tokens) {
+                    if (leader)
+                        mbar_expect_tx(bar, 4 * b_box);  // both CTAs' halves, two boxes each
+                    const uint32_t dst = smem_addr(bring + (size_t)stage * 2 * b_box);
+                    const uint32_t lead = mapa_rank(bar, 0);
+                    tma_load_2d(dst, &tm_x, kb * kTcK, trow, lead, pol);
+                    tma_load_2d(dst + b_box, &tm_x, kb * kTcK + 64, trow, lead, pol);
+                } else {
+                    mbar_expect_tx(bar, kTcWBytes);
+                    tma_load_2d(smem_addr(smem + (size_t)stage * kTcWBytes), &tm_w, kb * kTcK, vrow, bar, pol);
+                }
+                if (++stage == stages) {
                     stage = 0;
                     phase ^= 1u;
                 }
@@ -439,122 +487,137 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
         if (!ok)
             set_timeout(abort, a.flags);
         // copies already issued land before the pair meets at the last barrier
-        for (int s = 0; s < a.stages; ++s)
-            if (issued >> s & 1u) {
-                mbar_wait_final(smem_addr(&tail->wfull[s]), parity >> s & 1u);
-                if (leader)
-                    mbar_wait_final(smem_addr(&tail->bfull[s]), parity >> s & 1u);
-            }
-    } else if (warp == 1 && lane == 0 && leader) {
+        for (int s = 0; s < stages; ++s)
+            if ((issued >> s & 1u) && (leader || !tokens))
+                mbar_wait_final(smem_addr(&full[s]), parity >> s & 1u);
+    } else if (warp == 1 && leader) {
         // ---------------- MMA issuer (even CTA) ----------------
+        // The whole warp runs the loop and one lane issues: operands that are
+        // the same in every lane stay in uniform registers, where the
+        // instruction takes them (with a single thread in the loop, moving
+        // them there cost about 125 clocks per MMA, more than the MMA).
         int stage = 0, slot = 0, acc = 0;
         uint32_t phase = 0, aphase = 0, acc_phase = 0;
         bool ok = true;
+        const uint32_t bring_addr = smem_addr(bring);
+        const uint32_t full0 = smem_addr(&tail->bfull[0]), afull0 = smem_addr(&tail->afull[0]);
         for (int tile = tile0; tile < ntiles && ok; tile += tstep) {
-            if (!mbar_wait(smem_addr(&tail->tempty[acc]), acc_phase ^ 1u, abort, a.wait_ns)) {
+            ok = mbar_spin(smem_addr(&tail->tempty[acc]), acc_phase ^ 1u, abort, a.wait_ns);
+            if (!__all_sync(0xffffffffu, ok)) {
                 ok = false;
                 break;
             }
             const uint32_t d_tmem = tmem + (uint32_t)(acc * a.N);
-            for (int kb = 0; kb < kblocks; ++kb) {
-                if (!mbar_wait(smem_addr(&tail->bfull[stage]), phase, abort, a.wait_ns) ||
-                    !mbar_wait(smem_addr(&tail->afull[slot]), aphase, abort, a.wait_ns)) {
-                    ok = false;
-                    break;
-                }
-                tc_fence_after();
-                const uint32_t b_base = smem_addr(smem + (size_t)stage * stage_bytes) + kTcWBytes;
-                const uint32_t a_base = slot0 + (uint32_t)(slot * kTcSlotCols);
+            for (int kb = 0; kb < kblocks && ok; ++kb) {
+                ok = mbar_spin(full0 + stage * 8, phase, abort, a.wait_ns);
+                const uint64_t b_desc = k_major_sw128_desc(bring_addr + stage * 2 * b_box);
 #pragma unroll
-                for (int k = 0; k < kTcK / 16; ++k)
-                    mma_f16_ta(d_tmem, a_base + k * 8, k_major_sw128_desc(b_base + (k >> 2) * b_box + (k & 3) * 32),
-                               a.idesc, (kb | k) != 0);
-                mma_commit_mc(smem_addr(&tail->bempty[stage]));
-                mma_commit_mc(smem_addr(&tail->aempty[slot]));
-                if (++stage == a.stages) {
-                    stage = 0;
-                    phase ^= 1u;
+                for (int h = 0; h < 2; ++h) {
+                    ok = ok && mbar_spin(afull0 + (slot + h) * 8, aphase, abort, a.wait_ns);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok)
+                        break;
+                    tc_fence_after();
+                    const uint32_t a_base = slot0 + (uint32_t)((slot + h) * kTcSlotCols);
+                    const uint64_t desc = b_desc + (uint64_t)(h * (b_box >> 4));
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < kTcHalf / 16; ++k)
+                            mma_f16_ta(d_tmem, a_base + k * 8, desc + 2 * k, a.idesc, (kb | h | k) != 0);
+                        if (h == 1)
+                            mma_commit_mc(smem_addr(&tail->aempty[slot / 2]));
+                    }
+                    __syncwarp();
                 }
-                if (++slot == a.slots) {
+                slot += 2;
+                if (slot == a.slots) {
                     slot = 0;
                     aphase ^= 1u;
+                }
+                if (++stage == a.bstages) {
+                    stage = 0;
+                    phase ^= 1u;
                 }
             }
             if (!ok)
                 break;
-            mma_commit_mc(smem_addr(&tail->tfull[acc]));
+            if (elect_one())
+                mma_commit_mc(smem_addr(&tail->tfull[acc]));
+            __syncwarp();
             if (++acc == 2) {
                 acc = 0;
                 acc_phase ^= 1u;
             }
         }
-        if (!ok)
-            set_timeout(abort, a.flags);
-        mma_commit(smem_addr(&tail->drain));
-        mbar_wait_final(smem_addr(&tail->drain), 0);
+        if (elect_one()) {
+            if (!ok)
+                set_timeout(abort, a.flags);
+            mma_commit(smem_addr(&tail->drain));
+            mbar_wait_final(smem_addr(&tail->drain), 0);
+        }
+        __syncwarp();
     } else if (warp >= 8) {
         // ---------------- widening: the table's rows into tensor memory ----------------
         const int q = warp & 3;
         const int set = (warp - 8) >> 2;
         const int r = q * 32 + lane;
         const uint32_t lanes = (uint32_t)(q * 32) << 16;
-        int stage = 0, slot = 0;
+        int stage = 0, slot = set;  // the slots are even in number: a set keeps to its own
         uint32_t phase = 0, aphase = 0;
-        int turn = 0;
+        // a block's MMAs being done frees its slots and its stage of the tokens:
+        // the first widening warp passes the latter on
+        int seen = -a.slots / 2, bstage = 0;
         bool ok = true;
         for (int tile = tile0; tile < ntiles && ok; tile += tstep) {
             for (int kb = 0; kb < kblocks; ++kb) {
-                if (turn == set) {
-                    ok = mbar_wait(smem_addr(&tail->wfull[stage]), phase, abort, a.wait_ns);
-                    if (!__all_sync(0xffffffffu, ok)) {
-                        ok = false;
-                        break;
-                    }
-                    const unsigned char *row = smem + (size_t)stage * stage_bytes + r * 128;
-                    uint4 raw[8];
-#pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        raw[c] = *reinterpret_cast<const uint4 *>(row + ((c ^ (r & 7)) << 4));
-                    __syncwarp();
-                    if (lane == 0)
-                        mbar_arrive(smem_addr(&tail->wempty[stage]));
-                    ok = mbar_wait(smem_addr(&tail->aempty[slot]), aphase ^ 1u, abort, a.wait_ns);
-                    if (!__all_sync(0xffffffffu, ok)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t w[32];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const uint4 v = raw[h * 4 + c];
-                            const uint2 x0 = widen4(v.x), x1 = widen4(v.y), x2 = widen4(v.z), x3 = widen4(v.w);
-                            w[c * 8] = x0.x;
-                            w[c * 8 + 1] = x0.y;
-                            w[c * 8 + 2] = x1.x;
-                            w[c * 8 + 3] = x1.y;
-                            w[c * 8 + 4] = x2.x;
-                            w[c * 8 + 5] = x2.y;
-                            w[c * 8 + 6] = x3.x;
-                            w[c * 8 + 7] = x3.y;
-                        }
-                        tmem_store32(slot0 + (uint32_t)(slot * kTcSlotCols + h * 32) + lanes, w);
-                    }
-                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0)
-                        mbar_arrive_cluster(mapa_rank(smem_addr(&tail->afull[slot]), 0));
+                ok = mbar_spin(smem_addr(&tail->wfull[stage]), phase, abort, a.wait_ns);
+                if (!__all_sync(0xffffffffu, ok)) {
+                    ok = false;
+                    break;
                 }
-                turn ^= 1;
-                if (++stage == a.stages) {
+                const unsigned char *row = smem + (size_t)stage * kTcWBytes + r * 128;
+                uint4 raw[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    raw[c] = *reinterpret_cast<const uint4 *>(row + (((set * 4 + c) ^ (r & 7)) << 4));
+                uint32_t w[32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const unsigned x[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint2 p = widen4(x[e]);
+                        w[c * 8 + 2 * e] = p.x;
+                        w[c * 8 + 2 * e + 1] = p.y;
+                    }
+                }
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(smem_addr(&tail->wempty[stage]));
+                ok = mbar_spin(smem_addr(&tail->aempty[slot / 2]), aphase ^ 1u, abort, a.wait_ns);
+                if (!__all_sync(0xffffffffu, ok)) {
+                    ok = false;
+                    break;
+                }
+                if (++seen > 0 && warp == 8) {
+                    if (lane == 0)
+                        mbar_arrive(smem_addr(&tail->bempty[bstage]));
+                    bstage = bstage + 1 == a.bstages ? 0 : bstage + 1;
+                }
+                tc_fence_after();
+                tmem_store32(slot0 + (uint32_t)(slot * kTcSlotCols) + lanes, w);
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive_remote(mapa_rank(smem_addr(&tail->afull[slot]), 0));
+                if (++stage == a.wstages) {
                     stage = 0;
                     phase ^= 1u;
                 }
-                if (++slot == a.slots) {
-                    slot = 0;
+                slot += 2;
+                if (slot >= a.slots) {
+                    slot = set;
                     aphase ^= 1u;
                 }
             }
@@ -567,7 +630,7 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
         int acc = 0;
         uint32_t acc_phase = 0;
         for (int tile = tile0; tile < ntiles; tile += tstep) {
-            const bool ok = mbar_wait(smem_addr(&tail->tfull[acc]), acc_phase, abort, a.wait_ns);
+            const bool ok = mbar_spin(smem_addr(&tail->tfull[acc]), acc_phase, abort, a.wait_ns);
             if (!__all_sync(0xffffffffu, ok)) {
                 if (lane == 0 && !*abort)
                     set_timeout(abort, a.flags);
@@ -577,22 +640,22 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
             const int v = (tile / a.ntb * 2 + rank) * kTcRows + q * 32 + lane;
             const int t0 = tile % a.ntb * a.N;
             const float ws = v < a.V ? a.ws[v] : 0.f;
-            for (int ch = 0; ch < a.N / 32 && t0 + ch * 32 < a.T; ++ch) {
-                const int tc0 = t0 + ch * 32;
-                const float xs = tc0 + lane < a.T ? a.xs[tc0 + lane] : 0.f;
-                float d[32];
-                tmem_load32(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * a.N + ch * 32), d);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float x = __shfl_sync(0xffffffffu, xs, e);
-                    if (tc0 + e < a.T && v < a.V)
-                        store_out(a.out, a.obf16, (int64_t)(tc0 + e) * a.ldo + v, d[e] * x * ws);
-                }
-            }
+            const int nt = a.T - t0 < a.N ? a.T - t0 : a.N;  // tokens of this tile
+            float *xs = tail->xs[q];
+            for (int k = lane; k < a.N; k += 32)
+                xs[k] = k < nt ? a.xs[t0 + k] : 0.f;
+            __syncwarp();
+            const uint32_t d_tmem = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * a.N);
+            const int64_t at = (int64_t)t0 * a.ldo + v;
+            if (a.obf16)
+                write_tile(static_cast<unsigned short *>(a.out) + at, a.ldo, d_tmem, xs, ws, nt, v < a.V);
+            else
+                write_tile(static_cast<float *>(a.out) + at, a.ldo, d_tmem, xs, ws, nt, v < a.V);
+            __syncwarp();  // xs is read before the next tile writes it
             tc_fence_before();
             __syncwarp();
             if (lane == 0)
-                mbar_arrive_cluster(mapa_rank(smem_addr(&tail->tempty[acc]), 0));
+                mbar_arrive_remote(mapa_rank(smem_addr(&tail->tempty[acc]), 0));
             if (++acc == 2) {
                 acc = 0;
                 acc_phase ^= 1u;
@@ -650,13 +713,16 @@ cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *fla
     // as few token blocks as there can be, all of one width
     a.ntb = (int)((m.T + kTcMaxN - 1) / kTcMaxN);
     a.N = (int)(((m.T + a.ntb - 1) / a.ntb + 31) / 32 * 32);
-    a.slots = (512 - 2 * a.N) / kTcSlotCols;
+    a.slots = (512 - 2 * a.N) / kTcSlotCols;  // even: N is a multiple of 32
     if (a.slots > kTcMaxSlots)
         a.slots = kTcMaxSlots;
-    const size_t stage = kTcWBytes + (size_t)a.N * 128, fixed = 1024 + sizeof(TcTail);
-    a.stages = (int)((kTcSmem - fixed) / stage);
-    if (a.stages > kTcMaxStages)
-        a.stages = kTcMaxStages;
+    // shared memory: five blocks of the tokens (as long as they take to come
+    // from L2), the rest to the table
+    const size_t fixed = 1024 + sizeof(TcTail), bstage = (size_t)a.N * 128;
+    a.bstages = 5;
+    a.wstages = (int)((kTcSmem - fixed - a.bstages * bstage) / kTcWBytes);
+    if (a.wstages > kTcMaxStages)
+        a.wstages = kTcMaxStages;
     a.idesc = 1u << 4 | (uint32_t)(a.N >> 3) << 17 | (uint32_t)(2 * kTcRows >> 4) << 24;  // f32 += f16 f16, K-major
     CUtensorMap tm_w, tm_x;
     if (!make_load_map(&tm_w, m.wq, 1, m.K, m.V, m.ldw, kTcRows) ||
@@ -667,7 +733,7 @@ cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *fla
         return e;
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(kTcThreads);
-    cfg.dynamicSmemBytes = fixed + (size_t)a.stages * stage;
+    cfg.dynamicSmemBytes = fixed + a.bstages * bstage + (size_t)a.wstages * kTcWBytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -135,6 +135,30 @@ __device__ __forceinline__ float warp_max_nan(float v)
     return v;
 }
 
+// Pairs of floats in one instruction.
+struct f2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ f2 make2(float x, float y)
+{
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void split2(f2 a, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a.v)); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b)
+{
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b)
+{
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 inline bool dtype_ok(int t) { return t == EMBER_F32 || t == EMBER_BF16; }
 inline size_t elem_size(int t) { return t == EMBER_BF16 ? 2 : 4; }

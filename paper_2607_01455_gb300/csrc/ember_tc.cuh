@@ -67,6 +67,26 @@ __device__ inline bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *ab
     }
 }
 
+// The same for waits of whole warps in a loop: the clock and the abort word
+// are looked at every 32 tries only (a try suspends the thread for a while).
+__device__ __forceinline__ bool mbar_spin(uint32_t bar, uint32_t parity, volatile int *abort, uint64_t limit_ns)
+{
+    if (mbar_test(bar, parity))
+        return true;
+    uint64_t t0 = 0;
+    for (unsigned tries = 1;; ++tries) {
+        if (mbar_test(bar, parity))
+            return true;
+        if (tries % 32 == 0) {
+            const uint64_t t = dev::now_ns();
+            if (t0 == 0)
+                t0 = t;
+            if (*abort || t - t0 > limit_ns)
+                return false;
+        }
+    }
+}
+
 // Same, for teardown: no abort check, only the fixed limit kTeardownWaitNs (the
 // copies and MMAs already issued are waited for even when the main-loop
 // limit was made short).
@@ -159,6 +179,18 @@ __device__ __forceinline__ void cluster_arrive_release()
 }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
+// One lane of a converged warp, the same one every time.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
+}
+
 // Address of the same shared-memory variable in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t mapa_rank(uint32_t addr, uint32_t rank)
 {
@@ -189,6 +221,14 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                  "l"(src), "r"(bytes), "r"(bar)
                  : "memory");
+}
+
+// Arrive on a barrier of this or another CTA of the cluster, for waiters that
+// read tensor or shared memory alone: a release at cluster scope would first
+// wait for this thread's stores to global memory.
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
 // One box of the tensor map into this CTA's shared memory; its bytes complete on the
