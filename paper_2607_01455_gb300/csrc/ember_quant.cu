@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_mm_few(MmArgs a, int obf16, 
 //   - gets its 128 rows of the table as they are, 16 KiB of 8-bit integers, by
 //     TMA into 128-byte swizzled shared memory;
 //   - widens them to fp16 in registers (a thread per row and half, 64 values)
-//     and stores them in tensor memory as the A operand, in slots of 32
+//     and stores them in tensor memory as the A operand, in slots of 64
 //     columns: shared memory sees 8 bits per value of the table, not 8 + 16 + 16;
 //   - gets its half of the tokens' block, already fp16 (k_widen writes them
 //     once per call), by TMA.
@@ -247,10 +247,9 @@ constexpr int kTcRows = 128;        // rows of the table per CTA
 constexpr int kTcK = 128;           // block along K
 constexpr int kTcThreads = 512;
 constexpr int kTcMaxN = 192;        // two accumulators and two A slots fill tensor memory
-constexpr int kTcMaxStages = 10, kTcMaxSlots = 8;
+constexpr int kTcMaxStages = 10, kTcMaxSlots = 4;
 constexpr int kTcWBytes = kTcRows * kTcK;
-constexpr int kTcHalf = kTcK / 2;        // K of a slot of A
-constexpr int kTcSlotCols = kTcHalf / 2;  // fp16 pairs
+constexpr int kTcSlotCols = kTcK / 2;  // a block of A as fp16 pairs
 constexpr size_t kTcSmem = 227 << 10;
 
 struct TcTail {
@@ -259,7 +258,7 @@ struct TcTail {
     uint64_t bfull[kTcMaxStages];   // even CTA: both halves of the tokens landed
     uint64_t bempty[kTcMaxStages];  // each CTA: the MMAs of the stage are done (passed on by a widening warp)
     uint64_t afull[kTcMaxSlots];    // even CTA: both CTAs' A slots written
-    uint64_t aempty[kTcMaxSlots / 2];  // each CTA: the MMAs of a block, a pair of slots, are done
+    uint64_t aempty[kTcMaxSlots];   // each CTA: the MMAs of the slot are done
     uint64_t tfull[2], tempty[2];   // accumulators, as in the LM-head kernel
     uint64_t drain;
     uint32_t tmem_base;
@@ -414,9 +413,8 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
             mbar_init(smem_addr(&tail->bempty[s]), 1);
         }
         for (int s = 0; s < a.slots; ++s) {
-            mbar_init(smem_addr(&tail->afull[s]), 8);  // four warps in each CTA
-            if (s % 2 == 0)
-                mbar_init(smem_addr(&tail->aempty[s / 2]), 1);
+            mbar_init(smem_addr(&tail->afull[s]), 16);  // eight warps in each CTA
+            mbar_init(smem_addr(&tail->aempty[s]), 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_addr(&tail->tfull[s]), 1);
@@ -509,28 +507,23 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
             }
             const uint32_t d_tmem = tmem + (uint32_t)(acc * a.N);
             for (int kb = 0; kb < kblocks && ok; ++kb) {
-                ok = mbar_spin(full0 + stage * 8, phase, abort, a.wait_ns);
+                ok = mbar_spin(full0 + stage * 8, phase, abort, a.wait_ns) &&
+                     mbar_spin(afull0 + slot * 8, aphase, abort, a.wait_ns);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok)
+                    break;
+                tc_fence_after();
                 const uint64_t b_desc = k_major_sw128_desc(bring_addr + stage * 2 * b_box);
+                const uint32_t a_base = slot0 + (uint32_t)(slot * kTcSlotCols);
+                if (elect_one()) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    ok = ok && mbar_spin(afull0 + (slot + h) * 8, aphase, abort, a.wait_ns);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok)
-                        break;
-                    tc_fence_after();
-                    const uint32_t a_base = slot0 + (uint32_t)((slot + h) * kTcSlotCols);
-                    const uint64_t desc = b_desc + (uint64_t)(h * (b_box >> 4));
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = 0; k < kTcHalf / 16; ++k)
-                            mma_f16_ta(d_tmem, a_base + k * 8, desc + 2 * k, a.idesc, (kb | h | k) != 0);
-                        if (h == 1)
-                            mma_commit_mc(smem_addr(&tail->aempty[slot / 2]));
-                    }
-                    __syncwarp();
+                    for (int k = 0; k < kTcK / 16; ++k)
+                        mma_f16_ta(d_tmem, a_base + k * 8, b_desc + (uint64_t)((k >> 2) * (b_box >> 4) + 2 * (k & 3)),
+                                   a.idesc, (kb | k) != 0);
+                    mma_commit_mc(smem_addr(&tail->aempty[slot]));
                 }
-                slot += 2;
-                if (slot == a.slots) {
+                __syncwarp();
+                if (++slot == a.slots) {
                     slot = 0;
                     aphase ^= 1u;
                 }
@@ -562,11 +555,11 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
         const int set = (warp - 8) >> 2;
         const int r = q * 32 + lane;
         const uint32_t lanes = (uint32_t)(q * 32) << 16;
-        int stage = 0, slot = set;  // the slots are even in number: a set keeps to its own
+        int stage = 0, slot = 0;
         uint32_t phase = 0, aphase = 0;
         // a block's MMAs being done frees its slots and its stage of the tokens:
         // the first widening warp passes the latter on
-        int seen = -a.slots / 2, bstage = 0;
+        int seen = -a.slots, bstage = 0;
         bool ok = true;
         for (int tile = tile0; tile < ntiles && ok; tile += tstep) {
             for (int kb = 0; kb < kblocks; ++kb) {
@@ -594,7 +587,7 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
                 __syncwarp();
                 if (lane == 0)
                     mbar_arrive(smem_addr(&tail->wempty[stage]));
-                ok = mbar_spin(smem_addr(&tail->aempty[slot / 2]), aphase ^ 1u, abort, a.wait_ns);
+                ok = mbar_spin(smem_addr(&tail->aempty[slot]), aphase ^ 1u, abort, a.wait_ns);
                 if (!__all_sync(0xffffffffu, ok)) {
                     ok = false;
                     break;
@@ -605,7 +598,7 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
                     bstage = bstage + 1 == a.bstages ? 0 : bstage + 1;
                 }
                 tc_fence_after();
-                tmem_store32(slot0 + (uint32_t)(slot * kTcSlotCols) + lanes, w);
+                tmem_store32(slot0 + (uint32_t)(slot * kTcSlotCols + set * 32) + lanes, w);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
@@ -615,9 +608,8 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
                     stage = 0;
                     phase ^= 1u;
                 }
-                slot += 2;
-                if (slot >= a.slots) {
-                    slot = set;
+                if (++slot == a.slots) {
+                    slot = 0;
                     aphase ^= 1u;
                 }
             }
@@ -690,6 +682,26 @@ bool make_load_map(CUtensorMap *m, const void *base, int size, int64_t C, int64_
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Blocks of tokens, all of one width N (a multiple of 32).  One when they fit;
+// otherwise the widths from 192 down to 128 are weighed by the rounds that
+// the SM pairs need for the tiles and by what a round costs, its N and about
+// 24 tokens' worth of fixed work: narrower blocks leave less of the last round
+// idle and have more slots of A, wider ones read the table's tiles less often.
+void token_blocks(int64_t T, int64_t vblocks, int *ntb, int *N)
+{
+    int64_t best = INT64_MAX;
+    for (int n = kTcMaxN; n >= 128; n -= 32) {
+        const int64_t blocks = (T + n - 1) / n;
+        const int width = (int)(((T + blocks - 1) / blocks + 31) / 32 * 32);
+        const int64_t rounds = (vblocks * blocks + kSms / 2 - 1) / (kSms / 2);
+        if (rounds * (width + 24) < best) {
+            best = rounds * (width + 24);
+            *ntb = (int)blocks;
+            *N = width;
+        }
+    }
+}
+
 int64_t widened_cols(int64_t K) { return (K + 7) / 8 * 8; }
 
 cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *flags, cudaStream_t stream)
@@ -710,10 +722,8 @@ cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *fla
     a.K = m.K;
     a.obf16 = obf16;
     a.wait_ns = kDefaultWaitNs;
-    // as few token blocks as there can be, all of one width
-    a.ntb = (int)((m.T + kTcMaxN - 1) / kTcMaxN);
-    a.N = (int)(((m.T + a.ntb - 1) / a.ntb + 31) / 32 * 32);
-    a.slots = (512 - 2 * a.N) / kTcSlotCols;  // even: N is a multiple of 32
+    token_blocks(m.T, (m.V + 2 * kTcRows - 1) / (2 * kTcRows), &a.ntb, &a.N);
+    a.slots = (512 - 2 * a.N) / kTcSlotCols;
     if (a.slots > kTcMaxSlots)
         a.slots = kTcMaxSlots;
     // shared memory: five blocks of the tokens (as long as they take to come
