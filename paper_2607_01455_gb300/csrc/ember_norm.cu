@@ -68,26 +68,38 @@ __device__ __forceinline__ RowScale row_scale(float top)
     }
     return s;
 }
-__device__ __forceinline__ int quant(float y, const RowScale &s)
+// The low byte of the result is q: adding 1.5 2^23 leaves the value rounded to
+// an integer, nearest even, in the low bits of the fp32 number.  |y inv| is at
+// most 127 (1 + 2^-22), so no bound is needed there.
+__device__ __forceinline__ unsigned quant(float y, const RowScale &s)
 {
     if (s.divide)
-        return max(-127, min(127, __float2int_rn(y / s.scale)));
-    if (s.inv == 0.f)
-        return 0;
-    return max(-127, min(127, __float2int_rn(y * s.inv)));
+        y = fminf(fmaxf(y / s.scale, -127.f), 127.f);
+    return __float_as_uint(fmaf(y, s.divide ? 1.f : s.inv, 12582912.f));
 }
 
 template <int VEC>
 __device__ __forceinline__ void store_q(int8_t *p, const float (&y)[VEC], const RowScale &s)
 {
-    if constexpr (VEC == 8) {
-        unsigned u[2] = {0, 0};
+    unsigned q[VEC];
+    if (!s.divide && s.inv == 0.f) {  // zeros, also where y is infinite or NaN
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            u[e >> 2] |= (unsigned)(quant(y[e], s) & 0xff) << (8 * (e & 3));
+        for (int e = 0; e < VEC; ++e)
+            q[e] = 0;
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            q[e] = quant(y[e], s);
+    }
+    if constexpr (VEC == 8) {
+        unsigned u[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            u[k] = __byte_perm(__byte_perm(q[4 * k], q[4 * k + 1], 0x0040),
+                               __byte_perm(q[4 * k + 2], q[4 * k + 3], 0x0040), 0x5410);
         *reinterpret_cast<uint2 *>(p) = make_uint2(u[0], u[1]);
     } else
-        *p = (int8_t)quant(y[0], s);
+        *p = (int8_t)(q[0] & 0xff);
 }
 
 struct NormArgs {
@@ -102,8 +114,8 @@ struct NormArgs {
 enum { kOutSame = 0, kOutInt = 1 };
 
 // NORM = false: the rows themselves in 8 bits, without a norm.
-template <typename XT, typename RT, bool RES, bool NORM, int OUT, int VEC, int NV>
-__global__ void __launch_bounds__(1024) k_rmsnorm(NormArgs a)
+template <typename XT, typename RT, bool RES, bool NORM, int OUT, int VEC, int NV, int MAXT, int MINB>
+__global__ void __launch_bounds__(MAXT, MINB) k_rmsnorm(NormArgs a)
 {
     __shared__ float part[2][32];
     const int rpc = blockDim.x / a.tpr;
@@ -210,26 +222,249 @@ int threads_per_row(int64_t D, int vec, int nv)
     return t;
 }
 
-template <typename XT, typename RT, bool RES, bool NORM, int OUT, int VEC, int NV>
+template <typename XT, typename RT, bool RES, bool NORM, int OUT, int VEC, int NV, int MAXT = 1024, int MINB = 1>
 cudaError_t go_norm(NormArgs a, cudaStream_t stream)
 {
     a.tpr = threads_per_row(a.D, VEC, NV);
     const int block = a.tpr < kMinBlock ? kMinBlock : a.tpr;
     const int64_t rpc = block / a.tpr;
-    return launch_k(k_rmsnorm<XT, RT, RES, NORM, OUT, VEC, NV>, dim3((unsigned)((a.T + rpc - 1) / rpc)),
+    return launch_k(k_rmsnorm<XT, RT, RES, NORM, OUT, VEC, NV, MAXT, MINB>, dim3((unsigned)((a.T + rpc - 1) / rpc)),
                     dim3(block), 0, stream, true, a);
 }
 
+// Long rows of whole groups, one row per CTA at a time.  The rows come through
+// a ring of two in shared memory, filled by asynchronous copies; a thread
+// copies what it will read itself, so the ring needs no barrier, and the next
+// two rows are on their way while one is reduced and written.  A thread has the
+// same columns in every row and keeps their gains in registers.
+constexpr int kRing = 2;       // rows
+constexpr int kRingGroups = 4;  // groups of 8 per thread
+
+__device__ __forceinline__ void copy16(void *smem, const void *p)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p)
+                 : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// This thread's groups of one row of one input into the ring, and one of them back.
+template <typename T>
+__device__ __forceinline__ void ring_fetch(unsigned char *to, const T *row, int groups)
+{
+    constexpr int GB = 8 * sizeof(T);
+#pragma unroll
+    for (int k = 0; k < kRingGroups; ++k) {
+        const int g = k * blockDim.x + threadIdx.x;
+        if (g < groups) {
+#pragma unroll
+            for (int b = 0; b < GB; b += 16)
+                copy16(to + g * GB + b, reinterpret_cast<const unsigned char *>(row) + g * GB + b);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void ring_read(const unsigned char *from, int g, f2 (&f)[4])
+{
+    const unsigned char *p = from + g * (8 * sizeof(T));
+    Raw<T, 8> r;
+    if constexpr (sizeof(T) == 2)
+        r.v = *reinterpret_cast<const uint4 *>(p);
+    else {
+        r.a = reinterpret_cast<const float4 *>(p)[0];
+        r.b = reinterpret_cast<const float4 *>(p)[1];
+    }
+    unpack2<T>(r, f);
+}
+
+__device__ __forceinline__ void gains2(const void *gain, int gbf16, int groups, f2 (&ga)[kRingGroups][4])
+{
+#pragma unroll
+    for (int k = 0; k < kRingGroups; ++k) {
+        const int g = k * blockDim.x + threadIdx.x;
+        float e[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (g < groups)
+            load_gain<8>(gain, gbf16, g * 8, e);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            ga[k][q] = make2(e[2 * q], e[2 * q + 1]);
+    }
+}
+
+// A value per warp joined over the CTA; `part` is not written again before
+// another barrier.
+template <bool MAX>
+__device__ __forceinline__ float cta_join(float v, float *part)
+{
+    v = MAX ? warp_max_nan(v) : warp_sum(v);
+    const int nw = blockDim.x >> 5, lane = threadIdx.x & 31;
+    if (nw == 1)
+        return v;
+    if (lane == 0)
+        part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = lane < nw ? part[lane] : 0.f;
+    return MAX ? warp_max_nan(v) : warp_sum(v);
+}
+
+template <typename XT, typename RT, bool RES, int OUT, int MAXT, int MINB>
+__global__ void __launch_bounds__(MAXT, MINB) k_rmsnorm_ring(NormArgs a)
+{
+    extern __shared__ __align__(128) unsigned char ring[];  // [stage][x, residual]
+    __shared__ float part[2][2][32];                        // by parity of the row
+    const int tid = threadIdx.x, nt = blockDim.x;
+    const int groups = a.D / 8;
+    const int x_bytes = a.D * (int)sizeof(XT), row_bytes = x_bytes + (RES ? a.D * (int)sizeof(RT) : 0);
+    dev::grid_dep_wait();
+    dev::grid_dep_launch();
+    auto fetch = [&](int64_t row, int stage) {
+        if (row < a.T) {
+            unsigned char *to = ring + (size_t)stage * row_bytes;
+            ring_fetch<XT>(to, static_cast<const XT *>(a.x) + row * a.ldx, groups);
+            if constexpr (RES)
+                ring_fetch<RT>(to + x_bytes, static_cast<const RT *>(a.res) + row * a.ldr, groups);
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kRing; ++s)
+        fetch(blockIdx.x + (int64_t)s * gridDim.x, s);
+    f2 ga[kRingGroups][4];
+    gains2(a.gain, a.gbf16, groups, ga);
+    int stage = 0, par = 0;
+    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, par ^= 1) {
+        copies_wait<kRing - 1>();
+        const unsigned char *from = ring + (size_t)stage * row_bytes;
+        f2 s[kRingGroups][4];
+        f2 ss = make2(0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kRingGroups; ++k) {
+            const int g = k * nt + tid;
+            if (g < groups) {
+                ring_read<XT>(from, g, s[k]);
+                if constexpr (RES) {
+                    f2 r[4];
+                    ring_read<RT>(from + x_bytes, g, r);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        s[k][q] = add2(s[k][q], r[q]);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    s[k][q] = make2(0.f, 0.f);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                ss = fma2(s[k][q], s[k][q], ss);
+            if constexpr (RES) {
+                if (g < groups)
+                    store_group2<RT>(static_cast<RT *>(a.h) + row * a.ldh + g * 8, s[k]);
+            }
+        }
+        fetch(row + (int64_t)kRing * gridDim.x, stage);
+        stage = stage + 1 == kRing ? 0 : stage + 1;
+        const float rstd = 1.f / sqrtf(cta_join<false>(sum2(ss), part[par][0]) / (float)a.D + a.eps);
+        const f2 r2 = make2(rstd, rstd);
+#pragma unroll
+        for (int k = 0; k < kRingGroups; ++k)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                s[k][q] = mul2(mul2(s[k][q], r2), ga[k][q]);
+        if constexpr (OUT == kOutInt) {
+            float top = 0.f;
+#pragma unroll
+            for (int k = 0; k < kRingGroups; ++k)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float x, y;
+                    split2(s[k][q], x, y);
+                    top = max_nan(top, max_nan(fabsf(x), fabsf(y)));
+                }
+            const RowScale sc = row_scale(cta_join<true>(top, part[par][1]));
+#pragma unroll
+            for (int k = 0; k < kRingGroups; ++k) {
+                const int g = k * nt + tid;
+                if (g < groups) {
+                    float y[8];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        split2(s[k][q], y[2 * q], y[2 * q + 1]);
+                    store_q<8>(static_cast<int8_t *>(a.y) + row * a.ldy + g * 8, y, sc);
+                }
+            }
+            if (tid == 0)
+                a.scales[row] = sc.scale;
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRingGroups; ++k) {
+                const int g = k * nt + tid;
+                if (g < groups)
+                    store_group2<XT>(static_cast<XT *>(a.y) + row * a.ldy + g * 8, s[k]);
+            }
+        }
+    }
+    copies_wait<0>();
+}
+
+// Whether rows go through the ring, and with how many CTAs per SM: long rows
+// (a warp of kRingGroups groups a thread at least) whose ring fits the shared
+// memory.
+struct RingPlan {
+    bool on;
+    int block, per_sm;
+    size_t smem;
+};
+RingPlan ring_plan(int64_t D, int64_t row_bytes)
+{
+    RingPlan p{};
+    p.smem = (size_t)kRing * row_bytes;
+    p.block = threads_per_row(D, 8, kRingGroups);
+    p.on = D >= 1024 && D <= 16384 && p.smem <= 200 << 10;
+    p.per_sm = (int)((220 << 10) / (p.smem + 2048));
+    const int by_regs = 512 / p.block;
+    p.per_sm = p.per_sm < by_regs ? p.per_sm : by_regs;
+    p.per_sm = p.per_sm > 8 ? 8 : p.per_sm < 1 ? 1 : p.per_sm;
+    return p;
+}
+template <typename K, typename A>
+cudaError_t launch_ring(K kernel, const A &a, const RingPlan &p, int64_t grid, cudaStream_t stream)
+{
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10);
+    if (e != cudaSuccess)
+        return e;
+    return launch_k(kernel, dim3((unsigned)grid), dim3(p.block), p.smem, stream, true, a);
+}
+
 // Groups per thread: one while the rows alone do not fill the GPU (a call of
-// a few tokens is all latency), four otherwise (more loads in flight per
-// thread, fewer warps to join); rows off the 16-byte boundaries are taken
-// element by element.
+// a few tokens is all latency), four otherwise: two or eight were 10 to 60 %
+// slower on 65536 x 1024 to 8192 x 8192.  Rows off the 16-byte boundaries are
+// taken element by element.
+//   The ring where it pays, us for 67 M elements, ring / one row at a time:
+//   8 bits of x + residual  8192 columns 76 / 84, 4096 75 / 85, 1024 100 / 75;
+//   x alone in its type     8192 46 / 49, 4096 46 / 46, 1024 47 / 42;
+//   x + residual            8192 88 / 79 (all bf16): the simple form is at
+//                           the copy bandwidth already.
+//   Rows without a norm need few registers: six CTAs of 256 threads per SM (45
+// us for 8192 x 8192 bf16, 49 with four).
 template <typename XT, typename RT, bool RES, bool NORM, int OUT>
 cudaError_t pick_norm(const NormArgs &a, bool grouped8, cudaStream_t stream)
 {
     if (grouped8) {
         if (a.T <= kSms && a.D <= 8192)
             return go_norm<XT, RT, RES, NORM, OUT, 8, 1>(a, stream);
+        if constexpr (!NORM) {
+            if (a.D <= 8192)
+                return go_norm<XT, RT, RES, NORM, OUT, 8, 4, 256, 6>(a, stream);
+        } else if constexpr (OUT == kOutInt || !RES) {
+            const RingPlan p = ring_plan(a.D, a.D * (int64_t)(sizeof(XT) + (RES ? sizeof(RT) : 0)));
+            const int64_t grid = (int64_t)kSms * p.per_sm;
+            if (p.on && a.D > (OUT == kOutInt ? 1024 : 4096) && a.T >= 2 * grid)
+                return p.block <= 256
+                           ? launch_ring(k_rmsnorm_ring<XT, RT, RES, OUT, 256, 2>, a, p, grid, stream)
+                           : launch_ring(k_rmsnorm_ring<XT, RT, RES, OUT, 512, 1>, a, p, grid, stream);
+        }
         return go_norm<XT, RT, RES, NORM, OUT, 8, 4>(a, stream);
     }
     if (a.D <= 4096)
@@ -268,7 +503,7 @@ struct BackArgs {
 };
 
 template <typename XT, bool RES, int VEC, int NV, int MAXT>
-__global__ void __launch_bounds__(MAXT) k_rmsnorm_back(BackArgs a)
+__global__ void __launch_bounds__(MAXT, 1) k_rmsnorm_back(BackArgs a)
 {
     __shared__ float part[2][2][32];  // by parity of the row: one barrier per row
     const int rpc = blockDim.x / a.tpr;
@@ -369,26 +604,12 @@ __global__ void __launch_bounds__(MAXT) k_rmsnorm_back(BackArgs a)
     }
 }
 
-// The same for long rows of whole groups, one row per CTA at a time.  The rows
-// of dy, h and dres come through a ring of two rows in shared memory, filled by
-// asynchronous copies; a thread copies what it will read itself, so the ring
-// needs no barrier, and the next two rows are on their way while one is
-// reduced and written.
-constexpr int kBackStages = 2;
-
-__device__ __forceinline__ void copy16(void *smem, const void *p)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p)
-                 : "memory");
-}
-
+// The same for long rows of whole groups, through the ring of k_rmsnorm_ring.
 template <typename XT, bool RES, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) k_rmsnorm_back_ring(BackArgs a)
 {
-    constexpr int NV = 4;                   // groups of 8 per thread
-    constexpr int GB = 8 * sizeof(XT);      // bytes of a group
     constexpr int NIN = RES ? 3 : 2;
-    extern __shared__ __align__(128) unsigned char ring[];  // [stage][input][group of the row]
+    extern __shared__ __align__(128) unsigned char ring[];  // [stage][dy, h, dres]
     __shared__ float part[2][2][32];
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, w = tid >> 5, nw = nt >> 5;
     const int groups = a.D / 8;
@@ -398,70 +619,45 @@ __global__ void __launch_bounds__(MAXT, MINB) k_rmsnorm_back_ring(BackArgs a)
 
     auto fetch = [&](int64_t row, int stage) {
         if (row < a.T) {
-            const unsigned char *in[3] = {
-                reinterpret_cast<const unsigned char *>(static_cast<const XT *>(a.dy) + row * a.lddy),
-                reinterpret_cast<const unsigned char *>(static_cast<const XT *>(a.h) + row * a.ldh),
-                RES ? reinterpret_cast<const unsigned char *>(static_cast<const XT *>(a.dres) + row * a.lddres)
-                    : nullptr};
-#pragma unroll
-            for (int i = 0; i < NIN; ++i) {
-                unsigned char *to = ring + (size_t)(stage * NIN + i) * row_bytes;
-#pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    const int g = k * nt + tid;
-                    if (g < groups) {
-#pragma unroll
-                        for (int b = 0; b < GB; b += 16)
-                            copy16(to + g * GB + b, in[i] + g * GB + b);
-                    }
-                }
-            }
+            unsigned char *to = ring + (size_t)stage * NIN * row_bytes;
+            ring_fetch<XT>(to, static_cast<const XT *>(a.dy) + row * a.lddy, groups);
+            ring_fetch<XT>(to + row_bytes, static_cast<const XT *>(a.h) + row * a.ldh, groups);
+            if constexpr (RES)
+                ring_fetch<XT>(to + 2 * row_bytes, static_cast<const XT *>(a.dres) + row * a.lddres, groups);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        copies_commit();
     };
-    auto held = [&](int stage, int i, int g) {
-        const unsigned char *p = ring + (size_t)(stage * NIN + i) * row_bytes + g * GB;
-        Raw<XT, 8> r;
-        if constexpr (sizeof(XT) == 2)
-            r.v = *reinterpret_cast<const uint4 *>(p);
-        else {
-            r.a = reinterpret_cast<const float4 *>(p)[0];
-            r.b = reinterpret_cast<const float4 *>(p)[1];
-        }
-        return r;
-    };
-
-    float acc[NV][8];
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            acc[k][e] = 0.f;
-    const float inv_D = 1.f / (float)a.D;
-#pragma unroll
-    for (int s = 0; s < kBackStages; ++s)
+    for (int s = 0; s < kRing; ++s)
         fetch(blockIdx.x + (int64_t)s * gridDim.x, s);
+    f2 acc[kRingGroups][4], ga[kRingGroups][4];
+    gains2(a.gain, a.gbf16, groups, ga);
+#pragma unroll
+    for (int k = 0; k < kRingGroups; ++k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            acc[k][q] = make2(0.f, 0.f);
+    const float inv_D = 1.f / (float)a.D;
     int stage = 0, par = 0;
     for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, par ^= 1) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kBackStages - 1) : "memory");
-        float ss = 0.f, dot = 0.f;
+        copies_wait<kRing - 1>();
+        const unsigned char *from = ring + (size_t)stage * NIN * row_bytes;
+        f2 ss2 = make2(0.f, 0.f), dot2 = make2(0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
+        for (int k = 0; k < kRingGroups; ++k) {
             const int g = k * nt + tid;
             if (g < groups) {
-                float ga[8], fy[8], fh[8];
-                load_gain<8>(a.gain, a.gbf16, g * 8, ga);
-                unpack<XT, 8>(held(stage, 0, g), fy);
-                unpack<XT, 8>(held(stage, 1, g), fh);
+                f2 fy[4], fh[4];
+                ring_read<XT>(from, g, fy);
+                ring_read<XT>(from + row_bytes, g, fh);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    ss = fmaf(fh[e], fh[e], ss);
-                    dot = fmaf(fy[e] * ga[e], fh[e], dot);
+                for (int q = 0; q < 4; ++q) {
+                    ss2 = fma2(fh[q], fh[q], ss2);
+                    dot2 = fma2(mul2(fy[q], ga[k][q]), fh[q], dot2);
                 }
             }
         }
-        ss = warp_sum(ss);
-        dot = warp_sum(dot);
+        float ss = warp_sum(sum2(ss2)), dot = warp_sum(sum2(dot2));
         if (nw > 1) {
             if (lane == 0) {
                 part[par][0][w] = ss;
@@ -473,35 +669,35 @@ __global__ void __launch_bounds__(MAXT, MINB) k_rmsnorm_back_ring(BackArgs a)
         }
         const float r = 1.f / sqrtf(ss * inv_D + a.eps);
         const float c = r * r * (dot * inv_D);
+        const f2 r2 = make2(r, r), mc2 = make2(-c, -c);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
+        for (int k = 0; k < kRingGroups; ++k) {
             const int g = k * nt + tid;
             if (g < groups) {
-                float ga[8], fy[8], fh[8], o[8];
-                load_gain<8>(a.gain, a.gbf16, g * 8, ga);
-                unpack<XT, 8>(held(stage, 0, g), fy);
-                unpack<XT, 8>(held(stage, 1, g), fh);
+                f2 fy[4], fh[4], o[4];
+                ring_read<XT>(from, g, fy);
+                ring_read<XT>(from + row_bytes, g, fh);
                 if constexpr (RES)
-                    unpack<XT, 8>(held(stage, 2, g), o);
+                    ring_read<XT>(from + 2 * row_bytes, g, o);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = r * fmaf(-fh[e], c, fy[e] * ga[e]);
-                    o[e] = RES ? v + o[e] : v;
-                    acc[k][e] = fmaf(fy[e], fh[e] * r, acc[k][e]);
+                for (int q = 0; q < 4; ++q) {
+                    const f2 v = fma2(fh[q], mc2, mul2(fy[q], ga[k][q]));
+                    o[q] = RES ? fma2(v, r2, o[q]) : mul2(v, r2);
+                    acc[k][q] = fma2(fy[q], mul2(fh[q], r2), acc[k][q]);
                 }
-                store_group<XT, 8>(static_cast<XT *>(a.dx) + row * a.lddx + g * 8, o);
+                store_group2<XT>(static_cast<XT *>(a.dx) + row * a.lddx + g * 8, o);
             }
         }
-        fetch(row + (int64_t)kBackStages * gridDim.x, stage);
-        stage = stage + 1 == kBackStages ? 0 : stage + 1;
+        fetch(row + (int64_t)kRing * gridDim.x, stage);
+        stage = stage + 1 == kRing ? 0 : stage + 1;
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    copies_wait<0>();
     float *p = a.partial + (int64_t)blockIdx.x * a.D;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
+    for (int k = 0; k < kRingGroups; ++k) {
         const int g = k * nt + tid;
         if (g < groups)
-            store_group<float, 8>(p + g * 8, acc[k]);
+            store_group2<float>(p + g * 8, acc[k]);
     }
 }
 
@@ -527,35 +723,25 @@ __global__ void __launch_bounds__(1024) k_dgain(const float *__restrict__ partia
 }
 
 struct BackPlan {
+    RingPlan ring;
     int vec, nv, tpr, block, grid;
-    bool ring;
-    size_t smem;
     int64_t parts;  // partial rows
 };
 
-// Long rows of whole groups go through the ring: from 1024 columns on (a warp
-// of four groups a thread; shorter rows share a CTA), as long as two rows of
-// three inputs fit the shared memory.  The rest keeps one row in registers.
-BackPlan back_plan(int64_t T, int64_t D, int esize, bool grouped8)
+// Long rows of whole groups go through the ring; the rest keeps one row in
+// registers.
+BackPlan back_plan(int64_t T, int64_t D, int esize, bool res, bool grouped8)
 {
     BackPlan p{};
-    const size_t smem = (size_t)kBackStages * 3 * D * esize;
-    p.ring = grouped8 && D >= 1024 && smem <= 200 << 10;
+    p.ring = ring_plan(D, (res ? 3 : 2) * D * esize);
+    p.ring.on = p.ring.on && grouped8;
     p.vec = grouped8 ? 8 : 1;
-    p.nv = p.ring ? 4 : grouped8 ? (D <= 2048 ? 1 : D <= 8192 ? 2 : 4) : (D <= 4096 ? 4 : 32);
+    p.nv = grouped8 ? (D <= 2048 ? 1 : D <= 8192 ? 2 : 4) : (D <= 4096 ? 4 : 32);
     p.tpr = threads_per_row(D, p.vec, p.nv);
-    p.block = p.ring ? p.tpr : p.tpr < kMinBlock ? kMinBlock : p.tpr;
-    const int64_t rpc = p.block / p.tpr;
+    p.block = p.tpr < kMinBlock ? kMinBlock : p.tpr;
+    const int64_t rpc = p.ring.on ? 1 : p.block / p.tpr;
     const int64_t want = (T + rpc - 1) / rpc;
-    int per_sm = p.block >= 1024 ? 1 : 1024 / p.block;
-    if (p.ring) {
-        p.smem = smem;
-        per_sm = (int)((220 << 10) / (smem + 2048));
-        const int by_regs = 512 / p.block;
-        per_sm = per_sm < by_regs ? per_sm : by_regs;
-        per_sm = per_sm > 8 ? 8 : per_sm < 1 ? 1 : per_sm;
-    }
-    const int64_t most = (int64_t)kSms * per_sm;
+    const int64_t most = (int64_t)kSms * (p.ring.on ? p.ring.per_sm : p.block >= 1024 ? 1 : 1024 / p.block);
     p.grid = (int)(want < most ? want : most);
     p.parts = p.grid * rpc;
     return p;
@@ -565,14 +751,10 @@ template <typename XT, bool RES>
 cudaError_t launch_back(BackArgs a, const BackPlan &p, cudaStream_t stream)
 {
     a.tpr = p.tpr;
-    auto go = [&](auto kernel) { return launch_k(kernel, dim3(p.grid), dim3(p.block), p.smem, stream, true, a); };
-    if (p.ring) {
-        auto ring = [&](auto kernel) {
-            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10);
-            return e == cudaSuccess ? go(kernel) : e;
-        };
-        return p.block <= 256 ? ring(k_rmsnorm_back_ring<XT, RES, 256, 2>) : ring(k_rmsnorm_back_ring<XT, RES, 512, 1>);
-    }
+    if (p.ring.on)
+        return p.ring.block <= 256 ? launch_ring(k_rmsnorm_back_ring<XT, RES, 256, 2>, a, p.ring, p.grid, stream)
+                                   : launch_ring(k_rmsnorm_back_ring<XT, RES, 512, 1>, a, p.ring, p.grid, stream);
+    auto go = [&](auto kernel) { return launch_k(kernel, dim3(p.grid), dim3(p.block), 0, stream, true, a); };
     if (p.vec == 8) {
         if (p.nv == 1)
             return go(k_rmsnorm_back<XT, RES, 8, 1, 256>);
@@ -585,18 +767,22 @@ cudaError_t launch_back(BackArgs a, const BackPlan &p, cudaStream_t stream)
     return p.block <= 512 ? go(k_rmsnorm_back<XT, RES, 1, 32, 512>) : go(k_rmsnorm_back<XT, RES, 1, 32, 1024>);
 }
 
-// 8-bit rows back as what they stand for: q scale.
+// 8-bit rows back as what they stand for: q scale.  `tpr` threads a row, as
+// many rows as fit 256 threads; few rows are cut along their columns too.
 template <typename YT, int VEC>
 __global__ void __launch_bounds__(256) k_dequantize(const int8_t *__restrict__ q, int64_t ldq,
-                                                    const float *__restrict__ scales, int D, YT *__restrict__ y,
-                                                    int64_t ldy)
+                                                    const float *__restrict__ scales, int64_t T, int D, int tpr,
+                                                    YT *__restrict__ y, int64_t ldy)
 {
-    const int64_t row = blockIdx.x;
-    const int step = gridDim.y * blockDim.x * VEC;
+    const int64_t row = (int64_t)blockIdx.x * (256 / tpr) + threadIdx.x / tpr;
+    const int step = gridDim.y * tpr * VEC;
     dev::grid_dep_wait();
     dev::grid_dep_launch();
+    if (row >= T)
+        return;
     const float s = scales[row];
-    for (int col = (blockIdx.y * blockDim.x + threadIdx.x) * VEC; col < D; col += step) {
+#pragma unroll 4
+    for (int col = (blockIdx.y * tpr + threadIdx.x % tpr) * VEC; col < D; col += step) {
         float f[VEC];
         if constexpr (VEC == 8) {
             const uint2 u = *reinterpret_cast<const uint2 *>(q + row * ldq + col);
@@ -741,11 +927,15 @@ ember_status ember_dequantize_rows(const int8_t *q, int64_t ldq, const float *sc
     if (T == 0)
         return EMBER_OK;
     const bool grouped8 = D % 8 == 0 && aligned(q, 8) && ldq % 8 == 0 && grouped(y, ldy, ytype);
-    // four groups a thread in a long call; a few tokens' rows are spread over more CTAs
-    const int64_t per = (T <= kSms ? 256 : 1024) * (grouped8 ? 8 : 1);
-    const dim3 grid((unsigned)T, (unsigned)((D + per - 1) / per));
+    // four groups a thread in a long call, one otherwise
+    const int64_t groups = grouped8 ? D / 8 : D, per = T <= kSms ? 1 : 4;
+    int tpr = 32;
+    while (tpr < 256 && tpr * per < groups)
+        tpr *= 2;
+    const int64_t rpc = 256 / tpr, cols = T <= kSms ? (groups + tpr - 1) / tpr : 1;
+    const dim3 grid((unsigned)((T + rpc - 1) / rpc), (unsigned)cols);
     auto go = [&](auto kernel, auto *yt) {
-        return launch_k(kernel, grid, dim3(256), 0, (cudaStream_t)stream, true, q, ldq, scales, (int)D, yt, ldy);
+        return launch_k(kernel, grid, dim3(256), 0, (cudaStream_t)stream, true, q, ldq, scales, T, (int)D, tpr, yt, ldy);
     };
     if (ytype == EMBER_BF16)
         return launched(grouped8 ? go(k_dequantize<bf16_t, 8>, static_cast<bf16_t *>(y))
@@ -759,8 +949,8 @@ size_t ember_rmsnorm_backward_workspace_bytes(int64_t T, int64_t D)
     if (T < 0 || D < 1 || T > INT32_MAX || D > kMaxRowCols)
         return 0;
     int64_t most = 0;
-    for (int k = 0; k < 4; ++k) {
-        const int64_t n = back_plan(T, D, k & 1 ? 4 : 2, k >> 1).parts;
+    for (int k = 0; k < 8; ++k) {  // whatever the types, the alignment and dres
+        const int64_t n = back_plan(T, D, k & 1 ? 4 : 2, k & 2, k & 4).parts;
         most = most > n ? most : n;
     }
     return sizeof(float) * (size_t)(most * D);
@@ -786,7 +976,7 @@ ember_status ember_rmsnorm_backward(const void *dy, int64_t lddy, const void *h,
         return launched(cudaMemsetAsync(dgain, 0, sizeof(float) * (size_t)D, (cudaStream_t)stream));
     const bool grouped8 = D % 8 == 0 && grouped(dy, lddy, type) && grouped(h, ldh, type) &&
                           grouped(dres, lddres, type) && grouped(dx, lddx, type) && aligned(gain, 8 * elem_size(gtype));
-    const BackPlan p = back_plan(T, D, (int)elem_size(type), grouped8);
+    const BackPlan p = back_plan(T, D, (int)elem_size(type), dres != nullptr, grouped8);
     if (!workspace || bytes < sizeof(float) * (size_t)(p.parts * D))
         return EMBER_ERR_WORKSPACE;
     BackArgs a{};

@@ -159,6 +159,38 @@ __device__ __forceinline__ f2 mul2(f2 a, f2 b)
     return r;
 }
 
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
+{
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ float sum2(f2 a)
+{
+    float x, y;
+    split2(a, x, y);
+    return x + y;
+}
+// A group of 8 as pairs.
+template <typename T>
+__device__ __forceinline__ void unpack2(const Raw<T, 8> &r, f2 (&f)[4])
+{
+    float e[8];
+    unpack<T, 8>(r, e);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        f[k] = make2(e[2 * k], e[2 * k + 1]);
+}
+template <typename T>
+__device__ __forceinline__ void store_group2(T *p, const f2 (&f)[4])
+{
+    float e[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        split2(f[k], e[2 * k], e[2 * k + 1]);
+    store_group<T, 8>(p, e);
+}
+
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 inline bool dtype_ok(int t) { return t == EMBER_F32 || t == EMBER_BF16; }
 inline size_t elem_size(int t) { return t == EMBER_BF16 ? 2 : 4; }
