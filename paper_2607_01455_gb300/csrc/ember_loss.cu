@@ -11,7 +11,7 @@
 // (M, s e^(m-M) + s' e^(m'-M)), M = max(m, m').
 //
 // The pass is bound by HBM: each logit read once, each gradient written once.
-// A row of up to 262144 logits is spread over a cluster of up to 8 CTAs and
+// A row of up to 524288 logits is spread over a cluster of up to 16 CTAs and
 // stays in their registers between the statistics and the gradient; the CTAs
 // exchange one pair each through distributed shared memory.
 #include "ember_rows.cuh"
@@ -272,16 +272,21 @@ __device__ __forceinline__ float unit_max(const uint4 &r)
 }
 
 constexpr int kPerThread = 64;  // logits of a row per thread
-constexpr int kRowThreads = 256;  // two CTAs per SM; rows too long for them take twice as many, one CTA per SM
+constexpr int kMaxClusterRow = 16;  // CTAs of a row (a non-portable cluster size past 8)
+// Threads of a CTA: up to 256, several CTAs per SM; rows too long for 16 such
+// CTAs take twice as many, up to 512.
+constexpr int kRowThreads = 256;
 
 template <typename ZT, typename DT, bool GRAD, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT > kRowThreads ? 1 : 2) k_loss_rows(LossArgs a, int count_here)
+__global__ void __launch_bounds__(MAXT, (!GRAD && sizeof(ZT) == 2 ? 768 : 512) / MAXT)
+k_loss_rows(LossArgs a, int count_here)
 {
     constexpr int VE = Cut<ZT>::VE;
     constexpr int NU = kPerThread / VE;
+    constexpr bool kKeepExp = GRAD;  // e^(z - m0) is kept
     extern __shared__ __align__(128) unsigned char buf[];  // this CTA's slice of a row
     __shared__ MaxSum part[32];
-    __shared__ __align__(8) MaxSum all[2][8];
+    __shared__ __align__(8) MaxSum all[2][kMaxClusterRow];
     __shared__ int nvalid[32];
     __shared__ uint64_t full, joined[2];
     __shared__ int abort_;
@@ -298,8 +303,8 @@ __global__ void __launch_bounds__(MAXT, MAXT > kRowThreads ? 1 : 2) k_loss_rows(
         tc::mbar_init(tc::smem_addr(&joined[0]), 1);
         tc::mbar_init(tc::smem_addr(&joined[1]), 1);
         abort_ = 0;
-        for (int k = 0; k < 16; ++k)  // the places of CTAs that the cluster does not have stay so
-            all[k >> 3][k & 7] = {-kInf, 0.f};
+        for (int k = 0; k < 2 * kMaxClusterRow; ++k)  // the places of CTAs that the cluster does not have stay so
+            all[k / kMaxClusterRow][k % kMaxClusterRow] = {-kInf, 0.f};
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (C > 1)
@@ -405,21 +410,22 @@ __global__ void __launch_bounds__(MAXT, MAXT > kRowThreads ? 1 : 2) k_loss_rows(
         for (int k = 0; k < NU; ++k)
             mt = fmaxf(mt, unit_max<ZT>(r[k]));
         const float m0 = finite_max(mt);
-        float e[NU][VE];  // e^(z - m0)
+        float kept[kKeepExp ? NU : 1][VE];  // e^(z - m0)
         const float es = exp_of(zs - m0);
         f2 sum = make2(es, 0.f), sum2 = make2(0.f, 0.f);
         const f2 minus = make2(-m0, -m0), scale = make2(kLog2e, kLog2e);
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
-            unpack_unit<ZT, VE>(r[k], e[k]);
+            float(&e)[VE] = kept[kKeepExp ? k : 0];
+            unpack_unit<ZT, VE>(r[k], e);
 #pragma unroll
             for (int q = 0; q < VE; q += 2) {
-                const f2 x = mul2(add2(make2(e[k][q], e[k][q + 1]), minus), scale);
-                split2(x, e[k][q], e[k][q + 1]);
-                e[k][q] = exp2_of(e[k][q]);
-                e[k][q + 1] = exp2_of(e[k][q + 1]);
+                const f2 x = mul2(add2(make2(e[q], e[q + 1]), minus), scale);
+                split2(x, e[q], e[q + 1]);
+                e[q] = exp2_of(e[q]);
+                e[q + 1] = exp2_of(e[q + 1]);
                 f2 &to = q & 2 ? sum2 : sum;
-                to = add2(to, make2(e[k][q], e[k][q + 1]));
+                to = add2(to, make2(e[q], e[q + 1]));
             }
         }
         MaxSum ms;
@@ -447,7 +453,7 @@ __global__ void __launch_bounds__(MAXT, MAXT > kRowThreads ? 1 : 2) k_loss_rows(
             if (tid < C)
                 tc::store_remote_async(&all[p][rank], tid, ms.m, ms.s, jb);
             wait(jb, round >> 1 & 1u);
-            ms = lanes_join<8>(all[p][lane & 7]);
+            ms = lanes_join<kMaxClusterRow>(all[p][lane & (kMaxClusterRow - 1)]);
         }
         const float m = finite_max(ms.m);
         const bool live = on && ms.s != 0.f;
@@ -470,23 +476,24 @@ __global__ void __launch_bounds__(MAXT, MAXT > kRowThreads ? 1 : 2) k_loss_rows(
         if (single >= 0 && on && single == (int)y)
             a.nll[t] = live ? (m - zs) + logf(ms.s) : kInf;
         if constexpr (GRAD) {
-            // a row that does not count, or is -inf throughout, has only zeros in e
+            // a row that does not count, or is -inf throughout, has only zeros
             const f2 ff = make2(f, f);
 #pragma unroll
             for (int k = 0; k < NU; ++k) {
                 const int u = tid + k * nt;
+                float(&e)[VE] = kept[k];
 #pragma unroll
                 for (int q = 0; q < VE; q += 2)
-                    split2(mul2(make2(e[k][q], e[k][q + 1]), ff), e[k][q], e[k][q + 1]);
+                    split2(mul2(make2(e[q], e[q + 1]), ff), e[q], e[q + 1]);
                 if (u < c.n)
-                    store_unit<DT, VE>(d + c.head + (int64_t)(c.u0 + u) * VE, e[k]);
+                    store_unit<DT, VE>(d + c.head + (int64_t)(c.u0 + u) * VE, e);
             }
             if (mine) {
                 const float o[1] = {hot};
                 store_group<DT, 1>(d + y, o);
             }
             if (single >= 0) {
-                const float o[1] = {live ? es * f - (single == (int)y ? g : 0.f) : 0.f};
+                const float o[1] = {live ? exp_of(zs - m) * gs - (single == (int)y ? g : 0.f) : 0.f};
                 store_group<DT, 1>(d + single, o);
             }
         }
@@ -510,10 +517,10 @@ RowPlan row_plan(int64_t T, int64_t V, int esize)
     RowPlan p{0, 0, 0};
     const int64_t units = V / (16 / esize) + 1, nu = kPerThread / (16 / esize);
     int C = 1;
-    while (C < 8 && units > C * kRowThreads * nu)
+    while (C < kMaxClusterRow && units > C * kRowThreads * nu)
         C *= 2;
     const int64_t per = (units + C - 1) / C;
-    if (per > 2 * kRowThreads * nu || T * C > INT32_MAX)
+    if (per > 512 * nu || T * C > INT32_MAX)
         return p;
     p.C = C;
     p.nt = (int)((per + nu - 1) / nu + 31) / 32 * 32;
@@ -527,6 +534,8 @@ template <typename K>
 cudaError_t launch_cluster(K kernel, const LossArgs &a, const RowPlan &p, bool here, cudaStream_t stream)
 {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10);
+    if (e == cudaSuccess && p.C > 8)
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
@@ -572,9 +581,11 @@ cudaError_t launch_rows(const LossArgs &a, cudaStream_t stream)
         return e;
     if (p.C == 0)
         return launch_k(k_loss_stream<ZT, DT, GRAD>, dim3((unsigned)a.T), dim3(1024), 0, stream, true, a);
-    if (p.nt <= kRowThreads)
-        return launch_cluster(k_loss_rows<ZT, DT, GRAD, kRowThreads>, a, p, here, stream);
-    return launch_cluster(k_loss_rows<ZT, DT, GRAD, 2 * kRowThreads>, a, p, here, stream);
+    if (p.nt <= 128)
+        return launch_cluster(k_loss_rows<ZT, DT, GRAD, 128>, a, p, here, stream);
+    if (p.nt <= 256)
+        return launch_cluster(k_loss_rows<ZT, DT, GRAD, 256>, a, p, here, stream);
+    return launch_cluster(k_loss_rows<ZT, DT, GRAD, 512>, a, p, here, stream);
 }
 
 }  // namespace
