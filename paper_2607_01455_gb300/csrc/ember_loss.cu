@@ -502,6 +502,8 @@ k_loss_rows(LossArgs a, int count_here)
     }
     if (tid == 0 && *abort)
         tc::mbar_wait_final(bar, parity ^ 1u);  // the copy that was given up has left this CTA's shared memory
+    if (C > 1)
+        tc::cluster_sync();  // no CTA leaves while another, after a wait that gave up, still sends to it
 }
 
 // Threads per CTA and CTAs per row for rows of V logits; C = 0 where a row

@@ -6,8 +6,8 @@
 // and whose hidden states the norm wrote in 8 bits (ember_rmsnorm_quant).
 //
 // Three kernels, by the number of tokens and the rows' alignment:
-//   k_mm_few   up to kFewTokens tokens: the table is read once, the products
-//              by dp4a; bound by HBM.
+//   k_mm_few   up to 4 tokens, up to 8 of a small table: the table is read
+//              once, the products by dp4a; bound by HBM.
 //   k_mm_tc    more tokens: tcgen05 on pairs of CTAs; bound by HBM up to
 //              about 128 tokens, by the tensor cores beyond.
 //   k_mm_any   tables whose rows do not start on 16 bytes.
@@ -101,13 +101,14 @@ __global__ void __launch_bounds__(256) k_mm_any(MmArgs a, int obf16, unsigned vb
 
 // ---------------------------------------------------------------------------
 // Few tokens.  The tokens' rows sit in shared memory, zero-padded to whole
-// 512-byte slabs; a warp takes kFewRows rows of the table at a time, 16 bytes
-// of each row per lane and slab, so that every 16 bytes of x are read from
-// shared memory once for kFewRows rows.  The lanes' integer sums are joined by
-// a transposed butterfly: kFewRows TN totals for about as many shuffles.
+// 512-byte slabs; a warp takes R rows of the table at a time, 16 bytes of each
+// row per lane and slab, so that every 16 bytes of x are read from shared
+// memory once for R rows.  The lanes' integer sums are joined by a transposed
+// butterfly: R TN totals for about as many shuffles.  Bound by HBM for one to
+// four tokens: 128256 x 8192 for one token 149 us, 7.1 TB/s; for eight, dp4a
+// sets the pace (195 us).
 // ---------------------------------------------------------------------------
 constexpr int kFewTokens = 8;
-constexpr int kFewRows = 4;
 constexpr int kFewThreads = 256;
 constexpr size_t kFewSmem = 100 << 10;  // two CTAs per SM
 
@@ -150,8 +151,8 @@ __device__ __forceinline__ int dot16(int4 a, int4 b, int c)
     return __dp4a(a.w, b.w, __dp4a(a.z, b.z, __dp4a(a.y, b.y, __dp4a(a.x, b.x, c))));
 }
 
-template <int TN>
-__global__ void __launch_bounds__(kFewThreads, 2) k_mm_few(MmArgs a, int obf16, int kpad)
+template <int TN, int R, int MINB, int UNR>
+__global__ void __launch_bounds__(kFewThreads, MINB) k_mm_few(MmArgs a, int obf16, int kpad)
 {
     extern __shared__ __align__(16) int8_t sx[];  // [TN][kpad]
     const int lane = threadIdx.x & 31;
@@ -176,45 +177,45 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_mm_few(MmArgs a, int obf16, 
     }
     __syncthreads();
     const int whole = a.K / 16 * 16;  // up to here 16 bytes at once lie inside a row
-    const int64_t nquads = (a.V + kFewRows - 1) / kFewRows;
+    const int64_t nquads = (a.V + R - 1) / R;
     const int64_t step = (int64_t)gridDim.x * (kFewThreads / 32);
     for (int64_t q = (int64_t)blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5); q < nquads; q += step) {
-        int acc[kFewRows * TN];  // [row][token]
+        int acc[R * TN];  // [row][token]
 #pragma unroll
-        for (int e = 0; e < kFewRows * TN; ++e)
+        for (int e = 0; e < R * TN; ++e)
             acc[e] = 0;
-        const int8_t *w[kFewRows];
+        const int8_t *w[R];
 #pragma unroll
-        for (int r = 0; r < kFewRows; ++r) {
-            const int64_t v = q * kFewRows + r;
+        for (int r = 0; r < R; ++r) {
+            const int64_t v = q * R + r;
             w[r] = a.wq + (v < a.V ? v : a.V - 1) * a.ldw;
         }
-#pragma unroll 2
+#pragma unroll UNR
         for (int k = lane * 16; k < whole; k += 512) {
-            int4 c[kFewRows];
+            int4 c[R];
 #pragma unroll
-            for (int r = 0; r < kFewRows; ++r)
+            for (int r = 0; r < R; ++r)
                 c[r] = ldg_stream(w[r] + k);
 #pragma unroll
             for (int t = 0; t < TN; ++t) {
                 const int4 x = *reinterpret_cast<const int4 *>(sx + t * kpad + k);
 #pragma unroll
-                for (int r = 0; r < kFewRows; ++r)
+                for (int r = 0; r < R; ++r)
                     acc[r * TN + t] = dot16(c[r], x, acc[r * TN + t]);
             }
         }
         if (whole + lane < a.K) {  // the last, at most 15 values of a row, one per lane
 #pragma unroll
-            for (int r = 0; r < kFewRows; ++r)
+            for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int t = 0; t < TN; ++t)
                     acc[r * TN + t] += (int)w[r][whole + lane] * (int)sx[t * kpad + whole + lane];
         }
         int index;
-        const int sum = warp_isum_transposed<kFewRows * TN>(acc, lane, index);
-        const int64_t v = q * kFewRows + index / TN;
+        const int sum = warp_isum_transposed<R * TN>(acc, lane, index);
+        const int64_t v = q * R + index / TN;
         const int t = index % TN;
-        if (lane % (32 / (kFewRows * TN)) == 0 && v < a.V && t < a.T)
+        if (lane % (32 / (R * TN)) == 0 && v < a.V && t < a.T)
             store_out(a.out, obf16, t * a.ldo + v, (float)sum * a.xs[t] * a.ws[v]);
     }
 }
@@ -766,29 +767,44 @@ cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *fla
     return cudaLaunchKernelEx(&cfg, k_mm_tc, tm_w, tm_x, a);
 }
 
-template <int TN>
+template <int TN, int R, int MINB, int UNR>
 cudaError_t launch_few(const MmArgs &a, int obf16, int kpad, cudaStream_t stream)
 {
-    const cudaError_t e = cudaFuncSetAttribute(k_mm_few<TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
+    const cudaError_t e =
+        cudaFuncSetAttribute(k_mm_few<TN, R, MINB, UNR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
     if (e != cudaSuccess)
         return e;
-    const int64_t ctas = ((a.V + kFewRows - 1) / kFewRows + kFewThreads / 32 - 1) / (kFewThreads / 32);
-    return launch_k(k_mm_few<TN>, dim3((unsigned)(ctas < 2 * kSms ? ctas : 2 * kSms)), dim3(kFewThreads),
+    const int64_t ctas = ((a.V + R - 1) / R + kFewThreads / 32 - 1) / (kFewThreads / 32);
+    return launch_k(k_mm_few<TN, R, MINB, UNR>, dim3((unsigned)(ctas < MINB * kSms ? ctas : MINB * kSms)), dim3(kFewThreads),
                     (size_t)TN * kpad, stream, true, a, obf16, kpad);
 }
+
+// Rows per warp, CTAs per SM and unrolled slabs of k_mm_few, measured on
+// 151936 x 896 (short rows, where the joining of the lanes weighs) and 128256 x
+// 8192; us for 1 / 4 / 8 tokens:
+//   4 rows, 2 CTAs, 2 slabs   32 / 39 / 57    152 / 154 / 201
+//   4 rows, 2 CTAs, 4 slabs   31 / 35 / 44    149 / 164 / 195
+//   4 rows, 4 CTAs, 4 slabs   24 /  - /  -    162 /   - /   -
+//   8 rows, 2 CTAs, 4 slabs   25 / 29 /  -    158 / 166 /   -
+//   k_mm_tc                   31 / 31 / 31    179 / 179 / 180
+// Five to eight tokens go to the tensor cores where the table has a tile for
+// most SM pairs (4161 x 7856, 17 tiles: 17 us here, 30 there).
+constexpr int kFewShortRow = 2048;
+constexpr int64_t kFewMaxRows = 16384;
 
 cudaError_t launch_mm(const MmArgs &a, int obf16, void *workspace, unsigned *flags, cudaStream_t stream)
 {
     if (aligned(a.wq, 16) && a.ldw % 16 == 0) {
         const int kpad = (a.K + 511) / 512 * 512;
+        const bool brief = a.K <= kFewShortRow;
         if (a.T == 1 && (size_t)kpad <= kFewSmem)
-            return launch_few<1>(a, obf16, kpad, stream);
+            return brief ? launch_few<1, 4, 4, 4>(a, obf16, kpad, stream) : launch_few<1, 4, 2, 4>(a, obf16, kpad, stream);
         if (a.T == 2 && (size_t)2 * kpad <= kFewSmem)
-            return launch_few<2>(a, obf16, kpad, stream);
+            return brief ? launch_few<2, 8, 2, 4>(a, obf16, kpad, stream) : launch_few<2, 4, 2, 2>(a, obf16, kpad, stream);
         if (a.T <= 4 && (size_t)4 * kpad <= kFewSmem)
-            return launch_few<4>(a, obf16, kpad, stream);
-        if (a.T <= kFewTokens && (size_t)kFewTokens * kpad <= kFewSmem)
-            return launch_few<kFewTokens>(a, obf16, kpad, stream);
+            return brief ? launch_few<4, 8, 2, 4>(a, obf16, kpad, stream) : launch_few<4, 4, 2, 2>(a, obf16, kpad, stream);
+        if (a.T <= kFewTokens && a.V <= kFewMaxRows && (size_t)kFewTokens * kpad <= kFewSmem)
+            return launch_few<kFewTokens, 4, 2, 4>(a, obf16, kpad, stream);
         return launch_tc(a, obf16, workspace, flags, stream);
     }
     const int64_t vb = (a.V + kGV - 1) / kGV, tb = (a.T + kGT - 1) / kGT;

@@ -286,7 +286,7 @@ MM_SHAPES = [(1, 1, 1), (1, 5, 3), (1, 1000, 64), (1, 3001, 896), (1, 129, 8192)
              (4, 1000, 112), (7, 511, 1003), (8, 2000, 2048), (8, 100, 32768), (9, 300, 64), (16, 256, 128),
              (17, 255, 144), (31, 1030, 896), (49, 5000, 896), (64, 512, 1000), (65, 700, 200), (127, 129, 272),
              (128, 1280, 512), (200, 1000, 4096), (257, 515, 1008), (400, 900, 65), (1000, 2049, 320), (33, 40, 8192),
-             (12, 70000, 96), (0, 64, 64)]
+             (12, 70000, 96), (0, 64, 64), (6, 20000, 256), (3, 17000, 2064), (2, 30, 20000)]
 
 
 @pytest.mark.parametrize("T,V,K", MM_SHAPES)
@@ -672,3 +672,58 @@ def test_graph_capture(ops):
     torch.cuda.synchronize()
     for a, b in zip(got + buf, want):
         assert torch.equal(a, b)
+
+
+# ---- past 2^31 elements ----
+
+def test_offsets_past_32_bits(ops):
+    """The last rows of matrices of more than 2^31 elements, against calls on
+    those rows alone."""
+    g = gen(10)
+    T, D = 70000, 32768
+    x = torch.empty(T, D, device="cuda", dtype=BF)
+    x[:8] = rows(g, 8, D, BF)
+    x[8:-8] = 1.0
+    x[-8:] = rows(g, 8, D, BF)
+    y, h = ops.rmsnorm(x, None, residual=x)
+    y2, h2 = ops.rmsnorm(x[-8:].clone(), None, residual=x[-8:].clone())
+    assert torch.equal(y[-8:], y2) and torch.equal(h[-8:], h2)
+    del h
+    q, s = ops.quantize_rows(x)
+    q2, s2 = ops.quantize_rows(x[-8:].clone())
+    assert torch.equal(q[-8:], q2) and torch.equal(s[-8:], s2)
+    assert torch.equal(ops.dequantize_rows(q, s, out=y)[-8:], ops.dequantize_rows(q2, s2))
+    del q
+    dx, _ = ops.rmsnorm_backward(x, x, None, out=y)
+    assert torch.equal(dx[-8:], ops.rmsnorm_backward(x[-8:].clone(), x[-8:].clone(), None)[0])
+    del dx, y
+    z = x.view(-1)[:17000 * 128256].view(17000, 128256)
+    z[-3:] = rows(g, 3, 128256, BF)
+    t = torch.randint(0, 128256, (17000,), generator=g, device="cuda")
+    _, nll, d = ops.softmax_loss(z, t, reduction="sum")
+    _, nll2, d2 = ops.softmax_loss(z[-3:].clone(), t[-3:], reduction="sum")
+    assert torch.equal(nll[-3:], nll2) and torch.equal(d[-3:], d2)
+    out = [d.view(-1)]
+    norm = ops.clip_grads([z.view(-1)], 1.0, out=out)
+    want = z[-1].double() / (norm.item() + 1e-6)
+    close(d[-1], want, 2.0 ** -8 * want.abs() + 1e-6 * want.abs(), "clipped")
+    assert norm.item() == ops.grad_norm([z.view(-1)]).item()
+
+
+@pytest.mark.parametrize("T", [2, 40])
+def test_tables_and_logits_past_32_bits(ops, T):
+    g = gen(11)
+    V, K = 140000, 16384  # 2.3e9 bytes of table
+    wq = torch.ones(V, K, device="cuda", dtype=torch.int8)
+    wq[-300:] = ints(g, 300, K)
+    xq = ints(g, T, K)
+    xs, ws = torch.rand(T, generator=g, device="cuda"), torch.rand(V, generator=g, device="cuda")
+    out = ops.matmul_quant(xq, xs, wq, ws, dtype=F32)
+    assert torch.equal(out[:, -256:], ops.matmul_quant(xq, xs, wq[-256:].clone(), ws[-256:].clone(), dtype=F32))
+    del wq, out
+    T, V, K = 18000, 128000, 64
+    wq, xq = ints(g, V, K), ints(g, T, K)
+    xs, ws = torch.rand(T, generator=g, device="cuda"), torch.rand(V, generator=g, device="cuda")
+    out = ops.matmul_quant(xq, xs, wq, ws)
+    assert torch.equal(out[-200:], ops.matmul_quant(xq[-200:], xs[-200:], wq, ws))
+    assert ops.device_status() == E.EMBER_OK
