@@ -356,15 +356,18 @@ ember_status ember_set_wait_limit_ns(ember_handle *h, uint64_t ns);
  * row stride (ld..., in elements, at least the row length) and need the
  * alignment of their elements only; rows that start on 16 bytes take wider
  * accesses.  Scratch ("workspace", 16-byte aligned, contents irrelevant
- * before and after) belongs to the caller, as does the sticky status word
- * that some of them set where only the GPU can see an error.  Sums,
+ * before and after) belongs to the caller, as does the status block that
+ * some of them set where only the GPU can see an error.  Sums,
  * statistics and products are held in 32 bits or more and each output is
  * rounded once.  Results are the same bits on every run.
  * ------------------------------------------------------------------------- */
 
-/* A sticky status word: one unsigned in device memory.  init zeroes it on
- * `stream`; read synchronises the stream, returns EMBER_OK,
- * EMBER_ERR_ID_OUT_OF_RANGE or EMBER_ERR_TIMEOUT and clears it. */
+/* A status block: EMBER_STATUS_BYTES of device memory, 4-byte aligned, for
+ * calls that follow one another on the GPU (those of one stream).  init
+ * zeroes it on `stream`, once before its first use; read synchronises the
+ * stream, returns EMBER_OK, EMBER_ERR_ID_OUT_OF_RANGE or EMBER_ERR_TIMEOUT
+ * and clears it. */
+#define EMBER_STATUS_BYTES 16
 ember_status ember_status_init(unsigned *status, void *stream);
 ember_status ember_status_read(unsigned *status, void *stream);
 

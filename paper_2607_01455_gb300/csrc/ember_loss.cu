@@ -64,8 +64,10 @@ struct LossArgs {
     const float *w;
     void *d;
     float *nll, *loss;
-    long long *count;
-    unsigned *status;
+    int *count;     // counted tokens, a part per CTA of the counting kernel
+    double *total;  // parts of the loss
+    int nparts;
+    unsigned *status, *ticket;
     int64_t ldz, ldd, T, V, ignore;
     int y64, mean;
 };
@@ -78,45 +80,51 @@ __device__ __forceinline__ int64_t target_of(const LossArgs &a, int64_t t)
 // one does not, and is reported.
 __device__ __forceinline__ bool counts(const LossArgs &a, int64_t y) { return y != a.ignore && y >= 0 && y < a.V; }
 
-// The number of counted tokens, by one CTA.
+// The counted tokens of every kPartTokens or more.
+constexpr int kMaxParts = 64;
+constexpr int64_t kPartTokens = 2048;
 __global__ void __launch_bounds__(1024) k_loss_count(LossArgs a)
 {
-    __shared__ long long part[32];
+    __shared__ int part[32];
     dev::grid_dep_wait();
     dev::grid_dep_launch();
-    long long n = 0;
+    int n = 0;
     bool bad = false;
-    for (int64_t t = threadIdx.x; t < a.T; t += blockDim.x) {
+    for (int64_t t = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; t < a.T; t += (int64_t)gridDim.x * blockDim.x) {
         const int64_t y = target_of(a, t);
         n += counts(a, y);
         bad |= y != a.ignore && !counts(a, y);
     }
     if (bad)
         atomicOr(a.status, kFlagIdRange);
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1)
-        n += __shfl_xor_sync(0xffffffffu, n, o);
+    n = __reduce_add_sync(0xffffffffu, n);
     if ((threadIdx.x & 31) == 0)
         part[threadIdx.x >> 5] = n;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        n = 0;
-        for (int k = 0; k < 32; ++k)
-            n += part[k];
-        *a.count = n;
+    if (threadIdx.x < 32) {
+        n = __reduce_add_sync(0xffffffffu, part[threadIdx.x]);
+        if (threadIdx.x == 0)
+            a.count[blockIdx.x] = n;
     }
 }
-
-// The total, by one CTA: each thread adds its tokens in order, then a tree.
-__global__ void __launch_bounds__(1024) k_loss_total(LossArgs a)
+// Their number, by a whole warp.
+__device__ __forceinline__ int counted(const LossArgs &a)
 {
-    __shared__ double part[32];
-    dev::grid_dep_wait();
-    dev::grid_dep_launch();
+    int n = 0;
+    for (int k = threadIdx.x & 31; k < a.nparts; k += 32)
+        n += __ldcg(a.count + k);
+    return __reduce_add_sync(0xffffffffu, n);
+}
+
+// The losses of tokens first, first + step, ... by thread, added in order, then
+// a tree over the CTA; thread 0 gets the sum.  They were written by other
+// CTAs: they are read through L2.
+__device__ __forceinline__ double loss_sum(const LossArgs &a, int64_t first, int64_t step, double *part)
+{
     double s = 0.0;
-    for (int64_t t = threadIdx.x; t < a.T; t += blockDim.x)
+    for (int64_t t = first; t < a.T; t += step)
         if (counts(a, target_of(a, t)))
-            s += (double)a.nll[t] * (a.w ? (double)a.w[t] : 1.0);
+            s += (double)__ldcg(a.nll + t) * (a.w ? (double)a.w[t] : 1.0);
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1)
         s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -125,17 +133,49 @@ __global__ void __launch_bounds__(1024) k_loss_total(LossArgs a)
     __syncthreads();
     if (threadIdx.x == 0) {
         s = 0.0;
-        for (int k = 0; k < 32; ++k)
+        for (int k = 0; k < (int)(blockDim.x >> 5); ++k)
             s += part[k];
-        const long long n = a.mean ? *a.count : 1;
-        *a.loss = n > 0 ? (float)(s / (double)n) : 0.f;
     }
+    return s;
+}
+__device__ __forceinline__ void write_loss(const LossArgs &a, double s, int n)
+{
+    *a.loss = n == 0 ? 0.f : (float)(a.mean ? s / (double)n : s);
+}
+// Whether this CTA is the last of the grid to come here, what the others have
+// written then being visible; for every thread.
+__device__ __forceinline__ bool last_cta(const LossArgs &a, int *flag)
+{
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        *flag = atomicAdd(a.ticket, 1u) == gridDim.x - 1u;
+        __threadfence();
+        if (*flag)
+            *a.ticket = 0;
+    }
+    __syncthreads();
+    return *flag != 0;
 }
 
-__device__ __forceinline__ float row_gain(const LossArgs &a, int64_t t)
+// The total: a part per CTA, which the last one adds up in order.
+__global__ void __launch_bounds__(512) k_loss_total(LossArgs a)
 {
-    const float w = a.w ? a.w[t] : 1.f;
-    return a.mean ? w / (float)*a.count : w;
+    __shared__ double part[16];
+    __shared__ int last;
+    dev::grid_dep_wait();
+    dev::grid_dep_launch();
+    const double s = loss_sum(a, (int64_t)blockIdx.x * blockDim.x + threadIdx.x, (int64_t)gridDim.x * blockDim.x, part);
+    if (threadIdx.x == 0)
+        a.total[blockIdx.x] = s;
+    if (last_cta(a, &last) && threadIdx.x < 32) {
+        const int n = counted(a);
+        double sum = 0.0;
+        for (int k = 0; k < (int)gridDim.x; ++k)
+            sum += __ldcg(a.total + k);
+        if (threadIdx.x == 0)
+            write_loss(a, sum, n);
+    }
 }
 
 // One CTA per row, the row read twice (the second time from L2 when it is
@@ -183,7 +223,9 @@ __global__ void __launch_bounds__(1024) k_loss_stream(LossArgs a)
         a.nll[t] = ms.s == 0.f ? kInf : m - zy[0] + logf(ms.s);
     if (!GRAD)
         return;
-    const float g = row_gain(a, t);
+    float g = a.w ? a.w[t] : 1.f;
+    if (a.mean)
+        g /= (float)counted(a);
     const float f = ms.s == 0.f ? 0.f : g / ms.s;
     const float hot = ms.s == 0.f ? 0.f : g;
     for (int64_t v = threadIdx.x; v < a.V; v += blockDim.x) {
@@ -277,9 +319,9 @@ constexpr int kMaxClusterRow = 16;  // CTAs of a row (a non-portable cluster siz
 // CTAs take twice as many, up to 512.
 constexpr int kRowThreads = 256;
 
-template <typename ZT, typename DT, bool GRAD, int MAXT>
+template <typename ZT, typename DT, bool GRAD, bool HERE, int MAXT>
 __global__ void __launch_bounds__(MAXT, (!GRAD && sizeof(ZT) == 2 ? 768 : 512) / MAXT)
-k_loss_rows(LossArgs a, int count_here)
+k_loss_rows(LossArgs a)
 {
     constexpr int VE = Cut<ZT>::VE;
     constexpr int NU = kPerThread / VE;
@@ -287,7 +329,6 @@ k_loss_rows(LossArgs a, int count_here)
     extern __shared__ __align__(128) unsigned char buf[];  // this CTA's slice of a row
     __shared__ MaxSum part[32];
     __shared__ __align__(8) MaxSum all[2][kMaxClusterRow];
-    __shared__ int nvalid[32];
     __shared__ uint64_t full, joined[2];
     __shared__ int abort_;
     const int C = (int)tc::cluster_count_in(), rank = (int)tc::cluster_rank();
@@ -334,7 +375,8 @@ k_loss_rows(LossArgs a, int count_here)
     // the number of counted tokens: from the kernel before, or, when the
     // tokens are few, from their targets at once
     float n = 1.f;
-    if (count_here) {
+    if constexpr (HERE) {
+        __shared__ int nvalid[32];
         int c = 0;
         bool bad = false;
         for (int64_t q = tid; q < a.T; q += nt) {
@@ -356,7 +398,7 @@ k_loss_rows(LossArgs a, int count_here)
             *a.count = c;
     } else {
         if (a.mean)
-            n = (float)*a.count;
+            n = (float)counted(a);
         __syncthreads();  // the mbarriers are initialised
     }
 
@@ -462,10 +504,10 @@ k_loss_rows(LossArgs a, int count_here)
         const float g = w * inv_n;
         const float gs = __fdividef(g, ms.s);  // a sum is between 1 and 2^18: within two ulps
         const float f = live ? exp_of(m0 - m) * gs : 0.f;
-        // the target, by the thread that has it among its logits
+        // the target's loss and gradient, by the thread that has it among its logits
         const int yu = on ? (int)y - c.head - c.u0 * VE : -1;  // its place among this slice's logits
         const bool mine = yu >= 0 && yu < c.n * VE && yu / VE % nt == tid;
-        float hot = 0.f;  // its gradient
+        float hot = 0.f;
         if (mine) {
             // read again from the row: the copy's buffer may hold the next one already
             float zy[1];
@@ -502,6 +544,16 @@ k_loss_rows(LossArgs a, int count_here)
     }
     if (tid == 0 && *abort)
         tc::mbar_wait_final(bar, parity ^ 1u);  // the copy that was given up has left this CTA's shared memory
+    // few tokens: the last CTA to come here adds the losses up
+    if constexpr (HERE) {
+        __shared__ double dpart[16];
+        __shared__ int last;
+        if (last_cta(a, &last)) {
+            const double sum = loss_sum(a, tid, nt, dpart);
+            if (tid == 0)
+                write_loss(a, sum, __ldcg(a.count));
+        }
+    }
     if (C > 1)
         tc::cluster_sync();  // no CTA leaves while another, after a wait that gave up, still sends to it
 }
@@ -512,7 +564,11 @@ struct RowPlan {
     int C, nt;
     size_t smem;
 };
-constexpr int64_t kCountHere = 512;  // tokens whose targets every CTA counts itself
+// Up to so many tokens are one launch: every CTA counts the targets itself and
+// the last one adds up the losses (127 x 50257 fp32: 18.2 us, with launches of
+// their own for both 21.6).  More would keep a CTA busy for longer than the
+// launches take.
+constexpr int64_t kFewRowsHere = 512;
 
 RowPlan row_plan(int64_t T, int64_t V, int esize)
 {
@@ -533,7 +589,7 @@ RowPlan row_plan(int64_t T, int64_t V, int esize)
 // As many clusters as run at once, each with a share of the rows; one per row
 // when there are few.
 template <typename K>
-cudaError_t launch_cluster(K kernel, const LossArgs &a, const RowPlan &p, bool here, cudaStream_t stream)
+cudaError_t launch_cluster(K kernel, const LossArgs &a, const RowPlan &p, cudaStream_t stream)
 {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10);
     if (e == cudaSuccess && p.C > 8)
@@ -553,6 +609,7 @@ cudaError_t launch_cluster(K kernel, const LossArgs &a, const RowPlan &p, bool h
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
+    cfg.numAttrs = 2;
     if (a.T * p.C > kSms) {
         cfg.numAttrs = 1;
         int fit = 0;
@@ -561,33 +618,48 @@ cudaError_t launch_cluster(K kernel, const LossArgs &a, const RowPlan &p, bool h
             return e;
         if (fit < 1)
             return cudaErrorInvalidConfiguration;
+        // Clusters that share the rows are as many as an empty GPU holds, so
+        // they start on an empty one: let in while an earlier kernel still has
+        // an SM or two, they are placed around it, and one that then finds no
+        // room runs after all the others (4096 x 50257 bf16 295 us, 178 so).
         if (a.T > fit)
             cfg.gridDim = dim3((unsigned)fit * p.C);
+        else
+            cfg.numAttrs = 2;
     }
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a, (int)here);
+    return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <typename ZT, typename DT, bool GRAD>
-cudaError_t launch_rows(const LossArgs &a, cudaStream_t stream)
+cudaError_t launch_rows(LossArgs a, cudaStream_t stream)
 {
     RowPlan p = row_plan(a.T, a.V, sizeof(ZT));
     constexpr int VE = 16 / sizeof(ZT);
     if (GRAD && (((uintptr_t)a.z / sizeof(ZT) - (uintptr_t)a.d / sizeof(DT)) % VE != 0 || (a.ldz - a.ldd) % VE != 0))
         p.C = 0;
-    const bool here = p.C > 0 && a.T <= kCountHere;
+    const bool here = p.C > 0 && a.T <= kFewRowsHere;
+    a.nparts = here ? 1 : (int)(a.T / kPartTokens < kMaxParts ? a.T / kPartTokens + 1 : kMaxParts);
     cudaError_t e = cudaSuccess;
     if (!here)
-        e = launch_k(k_loss_count, dim3(1), dim3(1024), 0, stream, true, a);
+        e = launch_k(k_loss_count, dim3(a.nparts), dim3(1024), 0, stream, true, a);
     if (e != cudaSuccess)
         return e;
-    if (p.C == 0)
-        return launch_k(k_loss_stream<ZT, DT, GRAD>, dim3((unsigned)a.T), dim3(1024), 0, stream, true, a);
+    if (p.C == 0) {
+        e = launch_k(k_loss_stream<ZT, DT, GRAD>, dim3((unsigned)a.T), dim3(1024), 0, stream, true, a);
+        return e == cudaSuccess ? launch_k(k_loss_total, dim3(a.nparts), dim3(512), 0, stream, true, a) : e;
+    }
+    if (here)
+        return p.nt <= 256 ? launch_cluster(k_loss_rows<ZT, DT, GRAD, true, 256>, a, p, stream)
+                           : launch_cluster(k_loss_rows<ZT, DT, GRAD, true, 512>, a, p, stream);
     if (p.nt <= 128)
-        return launch_cluster(k_loss_rows<ZT, DT, GRAD, 128>, a, p, here, stream);
-    if (p.nt <= 256)
-        return launch_cluster(k_loss_rows<ZT, DT, GRAD, 256>, a, p, here, stream);
-    return launch_cluster(k_loss_rows<ZT, DT, GRAD, 512>, a, p, here, stream);
+        e = launch_cluster(k_loss_rows<ZT, DT, GRAD, false, 128>, a, p, stream);
+    else if (p.nt <= 256)
+        e = launch_cluster(k_loss_rows<ZT, DT, GRAD, false, 256>, a, p, stream);
+    else
+        e = launch_cluster(k_loss_rows<ZT, DT, GRAD, false, 512>, a, p, stream);
+    if (e == cudaSuccess)
+        e = launch_k(k_loss_total, dim3(a.nparts), dim3(512), 0, stream, true, a);
+    return e;
 }
 
 }  // namespace
@@ -599,7 +671,7 @@ extern "C" {
 
 size_t ember_softmax_loss_workspace_bytes(int64_t T)
 {
-    return T >= 0 && T <= INT32_MAX ? 256 : 0;
+    return T >= 0 && T <= INT32_MAX ? kMaxParts * (sizeof(double) + sizeof(int)) : 0;
 }
 
 ember_status ember_softmax_loss(const void *logits, int64_t ldz, ember_wdtype ztype, const void *targets,
@@ -629,8 +701,10 @@ ember_status ember_softmax_loss(const void *logits, int64_t ldz, ember_wdtype zt
     a.d = dlogits;
     a.nll = nll;
     a.loss = loss;
-    a.count = static_cast<long long *>(workspace);
+    a.total = static_cast<double *>(workspace);
+    a.count = reinterpret_cast<int *>(a.total + kMaxParts);
     a.status = status;
+    a.ticket = status + 1;
     a.ldz = ldz;
     a.ldd = ldd;
     a.T = T;
@@ -648,19 +722,18 @@ ember_status ember_softmax_loss(const void *logits, int64_t ldz, ember_wdtype zt
         e = db ? launch_rows<bf16_t, bf16_t, true>(a, s) : launch_rows<bf16_t, float, true>(a, s);
     else
         e = db ? launch_rows<float, bf16_t, true>(a, s) : launch_rows<float, float, true>(a, s);
-    if (e == cudaSuccess)
-        e = launch_k(k_loss_total, dim3(1), dim3(1024), 0, s, true, a);
     return launched(e);
 }
 
-// The sticky word of the operators that report what only the GPU sees.
+// The status block of the operators that report what only the GPU sees: the
+// sticky flags and a counter that each call leaves at zero.
 ember_status ember_status_init(unsigned *status, void *stream)
 {
     if (!status)
         return EMBER_ERR_INVALID_ARG;
     if (!aligned(status, 4))
         return EMBER_ERR_ALIGNMENT;
-    return launched(cudaMemsetAsync(status, 0, sizeof(unsigned), (cudaStream_t)stream));
+    return launched(cudaMemsetAsync(status, 0, EMBER_STATUS_BYTES, (cudaStream_t)stream));
 }
 
 ember_status ember_status_read(unsigned *status, void *stream)

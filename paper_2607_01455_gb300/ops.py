@@ -41,7 +41,7 @@ class _Refused(EmberError, ValueError):
 
 
 class Ops:
-    """The operators' workspace and sticky status word on one device, for use
+    """The operators' workspace and status block on one device, for use
     on one stream (calls on different streams share the workspace: give each
     stream its own object).  Before a graph capture, make each call once."""
 
@@ -54,6 +54,7 @@ class Ops:
         self._lib = lib()
         self._status = self._workspace = None  # made by the first call that needs them, on its stream
         self._kept = []
+        self._sizes = {}  # workspace bytes by operator and sizes
 
     # ---- arguments ----
 
@@ -89,7 +90,13 @@ class Ops:
             return None, EMBER_F32
         return self._vector(where, "gain", gain, D, _TYPES), _TYPES[gain.dtype]
 
-    def _scratch(self, nbytes):
+    def _scratch(self, bytes_of, *sizes):
+        """The workspace, of at least bytes_of(*sizes) bytes."""
+        nbytes = self._sizes.get((bytes_of, sizes))
+        if nbytes is None:
+            if len(self._sizes) >= 4096:
+                self._sizes.clear()
+            nbytes = self._sizes[bytes_of, sizes] = getattr(self._lib, bytes_of)(*sizes)
         w = self._workspace
         if w is None or w.numel() < nbytes:
             # a larger one, at least twice the size; the old one stays for the
@@ -102,7 +109,7 @@ class Ops:
 
     def _status_word(self):
         if self._status is None:
-            self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+            self._status = torch.zeros(4, dtype=torch.int32, device=self.device)  # EMBER_STATUS_BYTES
         return self._status.data_ptr()
 
     def _on(self, stream):
@@ -187,7 +194,7 @@ class Ops:
         pg, gt = self._gain(w, gain, D)
         dx, pd, ldd = self._result(w, out, shape, h.dtype)
         dgain = self._new(D, torch.float32)
-        ws = self._scratch(self._lib.ember_rmsnorm_backward_workspace_bytes(T, D))
+        ws = self._scratch("ember_rmsnorm_backward_workspace_bytes", T, D)
         _check(self._lib.ember_rmsnorm_backward(py, ldy, ph, ldh, pr, ldr, _TYPES[h.dtype], pg, gt, T, D, eps, pd, ldd,
                                                 dgain.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(self._index)), w)
         return dx, dgain
@@ -241,7 +248,7 @@ class Ops:
         if dtype not in _TYPES:
             raise _Refused(w, f"an output of type {dtype}", EMBER_ERR_DTYPE)
         o, po, ldo = self._result(w, out, (T, V), dtype)
-        work = self._scratch(self._lib.ember_matmul_quant_workspace_bytes(T, V, K))
+        work = self._scratch("ember_matmul_quant_workspace_bytes", T, V, K)
         _check(self._lib.ember_matmul_quant(px, ldx, pxs, pw, ldw, pws, T, V, K, po, ldo, _TYPES[dtype],
                                             work.data_ptr(), work.numel(), self._status_word(),
                                             _raw_stream(self._index)), w)
@@ -282,7 +289,7 @@ class Ops:
                 pd, ldd = self._matrix(w, "out", d, (dt,), logits.shape)
         loss = self._new((), torch.float32)
         nll = self._new(T, torch.float32)
-        work = self._scratch(self._lib.ember_softmax_loss_workspace_bytes(T))
+        work = self._scratch("ember_softmax_loss_workspace_bytes", T)
         _check(self._lib.ember_softmax_loss(pz, ldz, _TYPES[logits.dtype], py, _IDS[targets.dtype], pw, ignore_index,
                                             int(reduction == "mean"), T, V, loss.data_ptr(), nll.data_ptr(), pd, ldd,
                                             _TYPES[dt], work.data_ptr(), work.numel(), self._status_word(),
@@ -293,26 +300,25 @@ class Ops:
 
     def _list(self, where, tensors, out):
         """The host arrays of a call over many tensors: addresses, sizes, types."""
-        for t in tensors:
-            if t.get_device() != self._index or not t.is_contiguous():
-                raise _Refused(where, f"a gradient of shape {tuple(t.shape)}, strides {t.stride()} on {t.device}: "
-                                      f"contiguous tensors on {self.device} are needed")
-        kinds = [t.dtype for t in tensors]
-        try:
-            types = array("i", [_TYPES[d] for d in kinds])
-        except KeyError as e:
-            raise _Refused(where, f"a gradient of type {e.args[0]}", EMBER_ERR_DTYPE) from None
+        n = len(tensors)
+        here = [self._index] * n
+        types = [_TYPES.get(t.dtype) for t in tensors]
+        if [t.get_device() for t in tensors] != here or not all([t.is_contiguous() for t in tensors]):
+            raise _Refused(where, f"gradients that are not contiguous tensors on {self.device}: "
+                                  f"{[(tuple(t.shape), t.stride(), str(t.device)) for t in tensors][:8]}")
+        if None in types:
+            raise _Refused(where, f"a gradient of type {tensors[types.index(None)].dtype}", EMBER_ERR_DTYPE)
         numel = array("q", [t.numel() for t in tensors])
         ptrs = array("Q", [t.data_ptr() for t in tensors])
         if out is None:
-            return ptrs, ptrs, numel, types
-        if len(out) != len(tensors):
-            raise _Refused(where, f"{len(out)} outputs for {len(tensors)} gradients")
-        for t, o, d in zip(tensors, out, kinds):
-            if o.shape != t.shape or o.dtype != d or o.get_device() != self._index or not o.is_contiguous():
-                raise _Refused(where, f"an output of shape {tuple(o.shape)}, type {o.dtype} for a gradient of "
-                                      f"shape {tuple(t.shape)}, type {t.dtype}")
-        outs = array("Q", [o.data_ptr() for o in out])
+            return ptrs, ptrs, numel, array("i", types)
+        if len(out) != n:
+            raise _Refused(where, f"{len(out)} outputs for {n} gradients")
+        if ([o.shape for o in out] != [t.shape for t in tensors] or [_TYPES.get(o.dtype) for o in out] != types
+                or [o.get_device() for o in out] != here or not all([o.is_contiguous() for o in out])):
+            raise _Refused(where, f"an output of shape, type or device other than its gradient's, or not contiguous: "
+                                  f"{[(tuple(o.shape), str(o.dtype), str(o.device)) for o in out][:8]}")
+        outs, types = array("Q", [o.data_ptr() for o in out]), array("i", types)
         return ptrs, outs, numel, types
 
     def grad_norm(self, tensors, stream=None):
@@ -325,7 +331,7 @@ class Ops:
         ptrs, _, numel, types = self._list(w, tensors, None)
         norm = self._new((), torch.float32)
         n = len(tensors)
-        work = self._scratch(self._lib.ember_clip_workspace_bytes(n))
+        work = self._scratch("ember_clip_workspace_bytes", n)
         _check(self._lib.ember_grad_norm(n, ptrs.buffer_info()[0], numel.buffer_info()[0], types.buffer_info()[0],
                                          norm.data_ptr(), work.data_ptr(), work.numel(), _raw_stream(self._index)), w)
         return norm
@@ -342,7 +348,7 @@ class Ops:
         ptrs, outs, numel, types = self._list(w, tensors, out)
         norm = self._new((), torch.float32)
         n = len(tensors)
-        work = self._scratch(self._lib.ember_clip_workspace_bytes(n))
+        work = self._scratch("ember_clip_workspace_bytes", n)
         _check(self._lib.ember_clip_grads(n, ptrs.buffer_info()[0], outs.buffer_info()[0], numel.buffer_info()[0],
                                           types.buffer_info()[0], max_norm, eps, norm.data_ptr(), work.data_ptr(),
                                           work.numel(), _raw_stream(self._index)), w)
