@@ -371,6 +371,13 @@ ember_status ember_set_wait_limit_ns(ember_handle *h, uint64_t ns);
 ember_status ember_status_init(unsigned *status, void *stream);
 ember_status ember_status_read(unsigned *status, void *stream);
 
+/* Limit, in nanoseconds of wall time, of the bounded waits inside the kernels
+ * of ember_matmul_quant and ember_softmax_loss, for the calls of this process
+ * from now on; 0 restores the default of 2 s.  A wait that runs past it sets
+ * EMBER_ERR_TIMEOUT in the status block, and the kernel returns early with
+ * its outputs incomplete.  Host only. */
+ember_status ember_set_ops_wait_limit(uint64_t ns);
+
 /* Residual addition and root-mean-square norm of T rows of D values:
  *   s = x + residual,  h = s,  y_j = gain_j s_j / sqrt(mean_j s_j^2 + eps).
  *   x:        T x D of xtype; y (T x D, xtype) is written and may be x.

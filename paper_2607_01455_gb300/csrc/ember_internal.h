@@ -221,6 +221,9 @@ inline int reduce_rows_per_thread(int64_t V, int64_t D, const ColMap &m)
 // mbarrier waits): 2 s of wall time.
 constexpr uint64_t kDefaultWaitNs = 2000000000ull;
 
+// The limit of the operators without a handle (ember_set_ops_wait_limit).
+uint64_t ops_wait_ns();
+
 cudaError_t launch_dense_step(const DenseArgs &a);
 
 // beta2 r + (1 - beta2) m is formed in fp32 with each coefficient carried as

@@ -14,6 +14,8 @@
 // A row of up to 524288 logits is spread over a cluster of up to 16 CTAs and
 // stays in their registers between the statistics and the gradient; the CTAs
 // exchange one pair each through distributed shared memory.
+#include <atomic>
+
 #include "ember_rows.cuh"
 #include "ember_tc.cuh"
 
@@ -68,6 +70,7 @@ struct LossArgs {
     double *total;  // parts of the loss
     int nparts;
     unsigned *status, *ticket;
+    uint64_t wait_ns;
     int64_t ldz, ldd, T, V, ignore;
     int y64, mean;
 };
@@ -252,9 +255,8 @@ __global__ void __launch_bounds__(1024) k_loss_stream(LossArgs a)
 // the first CTA.  The gradient's rows are at the same places of their units
 // (launch_rows sees to it).
 //
-// A wait that gives up sets the timeout flag; from then on the CTA starts no
-// copy and waits for nothing, and runs its rows to their end, still sending
-// its pairs.
+// A wait that gives up sets the timeout flag and ends its CTA's rows; the
+// other CTAs of the cluster, which then lack its pairs, give up likewise.
 template <typename T, int N>
 __device__ __forceinline__ void unpack_unit(const uint4 &r, float (&f)[N])
 {
@@ -354,16 +356,21 @@ k_loss_rows(LossArgs a)
     dev::grid_dep_launch();
 
     // The copy of row t's slice, by thread 0; rows that do not count need none.
+    uint32_t started = 0;
     auto start = [&](int64_t t, int64_t y) {
         const ZT *z = zbase + t * a.ldz;
         const Cut<ZT> q(z, V, log_C, rank);
         if (!counts(a, y) || q.n == 0)
             return;
+        ++started;
         tc::mbar_expect_tx(bar, (uint32_t)q.n * 16);
         tc::bulk_load(tc::smem_addr(buf), z + q.head + (int64_t)q.u0 * VE, (uint32_t)q.n * 16, bar);
     };
+    bool failed = false;  // a wait of this thread gave up
+    bool met = false;     // the first cluster barrier is behind this CTA
     auto wait = [&](uint32_t b, uint32_t parity) {
-        if (!*abort && !tc::mbar_spin(b, parity, abort, kDefaultWaitNs)) {
+        if (!failed && !tc::mbar_spin(b, parity, abort, a.wait_ns)) {
+            failed = true;
             atomicOr(a.status, kFlagTimeout);
             *abort = 1;
         }
@@ -443,8 +450,9 @@ k_loss_rows(LossArgs a)
                 r[k] = tid + k * nt < have ? reinterpret_cast<const uint4 *>(buf)[tid + k * nt]
                                            : make_uint4(fill, fill, fill, fill);
         }
-        __syncthreads();
-        if (tid == 0 && more && !*abort)
+        if (__syncthreads_or(failed))
+            break;
+        if (tid == 0 && more)
             start(t + step, ynext);
 
         float mt = zs;
@@ -487,6 +495,7 @@ k_loss_rows(LossArgs a)
         if (C > 1) {
             if (round == 0)
                 tc::cluster_wait();
+            met = true;
             // every CTA's pair into every CTA
             const uint32_t p = round & 1u;
             const uint32_t jb = tc::smem_addr(&joined[p]);
@@ -542,8 +551,18 @@ k_loss_rows(LossArgs a)
         y = ynext;
         ynext = yafter;
     }
-    if (tid == 0 && *abort)
-        tc::mbar_wait_final(bar, parity ^ 1u);  // the copy that was given up has left this CTA's shared memory
+    const bool gave_up = __syncthreads_or(failed);
+    if (C > 1 && !met)
+        tc::cluster_wait();
+    if (gave_up && tid == 0) {
+        // what is in flight has landed before the CTA ends: the copy it started
+        // last, and the other CTAs' pairs (they take about a microsecond)
+        if (started)
+            tc::mbar_wait_final(bar, (started - 1u) & 1u);
+        const uint64_t t0 = dev::now_ns();
+        while (dev::now_ns() - t0 < 100000)
+            ;
+    }
     // few tokens: the last CTA to come here adds the losses up
     if constexpr (HERE) {
         __shared__ double dpart[16];
@@ -555,7 +574,7 @@ k_loss_rows(LossArgs a)
         }
     }
     if (C > 1)
-        tc::cluster_sync();  // no CTA leaves while another, after a wait that gave up, still sends to it
+        tc::cluster_sync();  // no CTA leaves while another may still send to it
 }
 
 // Threads per CTA and CTAs per row for rows of V logits; C = 0 where a row
@@ -667,6 +686,9 @@ cudaError_t launch_rows(LossArgs a, cudaStream_t stream)
 
 using namespace ember;
 
+static std::atomic<uint64_t> ops_wait{kDefaultWaitNs};
+uint64_t ember::ops_wait_ns() { return ops_wait.load(std::memory_order_relaxed); }
+
 extern "C" {
 
 size_t ember_softmax_loss_workspace_bytes(int64_t T)
@@ -705,6 +727,7 @@ ember_status ember_softmax_loss(const void *logits, int64_t ldz, ember_wdtype zt
     a.count = reinterpret_cast<int *>(a.total + kMaxParts);
     a.status = status;
     a.ticket = status + 1;
+    a.wait_ns = ops_wait_ns();
     a.ldz = ldz;
     a.ldd = ldd;
     a.T = T;
@@ -734,6 +757,12 @@ ember_status ember_status_init(unsigned *status, void *stream)
     if (!aligned(status, 4))
         return EMBER_ERR_ALIGNMENT;
     return launched(cudaMemsetAsync(status, 0, EMBER_STATUS_BYTES, (cudaStream_t)stream));
+}
+
+ember_status ember_set_ops_wait_limit(uint64_t ns)
+{
+    ops_wait.store(ns ? ns : kDefaultWaitNs, std::memory_order_relaxed);
+    return EMBER_OK;
 }
 
 ember_status ember_status_read(unsigned *status, void *stream)

@@ -241,6 +241,8 @@ __global__ void __launch_bounds__(kFewThreads, MINB) k_mm_few(MmArgs a, int obf1
 //   warps 8-15  widen: two sets of four warps, one per half of a block
 // Every wait is bounded; one that gives up sets the timeout flag, stops every
 // role, and the kernel returns after its copies and MMAs in flight are done.
+// The two CTAs may then have issued different numbers of copies of the tokens,
+// whose bytes complete on one barrier: the even CTA evens the counts out.
 // ---------------------------------------------------------------------------
 using namespace tc;
 
@@ -264,6 +266,8 @@ struct TcTail {
     uint64_t drain;
     uint32_t tmem_base;
     int abort;
+    int64_t issued[2];   // in the even CTA: blocks of the tokens whose copies each CTA has issued
+    int64_t gave_up[2];  // in both: whether a wait of either CTA gave up
     float xs[4][kTcMaxN];  // the tokens' scales of a tile, a copy per epilogue warp
 };
 
@@ -450,7 +454,7 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
         uint64_t *full = tokens ? tail->bfull : tail->wfull, *empty = tokens ? tail->bempty : tail->wempty;
         int stage = 0;
         uint32_t phase = 0;
-        uint32_t issued = 0, parity = 0;  // a bit per stage: a copy was issued, the parity of its last phase
+        int64_t issued = 0;  // blocks whose copies were issued
         asm volatile("fence.proxy.async.global;" ::: "memory");  // the tokens were written by plain stores
         // the table streams when every block is read once
         const uint64_t pol = l2_policy(tokens ? 1 : a.ntb > 1 ? 0 : 2);
@@ -464,8 +468,7 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
                     break;
                 }
                 const uint32_t bar = smem_addr(&full[stage]);
-                issued |= 1u << stage;
-                parity = (parity & ~(1u << stage)) | phase << stage;
+                ++issued;
                 if (tokens) {
                     if (leader)
                         mbar_expect_tx(bar, 4 * b_box);  // both CTAs' halves, two boxes each
@@ -485,10 +488,11 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
         }
         if (!ok)
             set_timeout(abort, a.flags);
-        // copies already issued land before the pair meets at the last barrier
-        for (int s = 0; s < stages; ++s)
-            if ((issued >> s & 1u) && (leader || !tokens))
-                mbar_wait_final(smem_addr(&full[s]), parity >> s & 1u);
+        if (tokens)
+            store_remote_i64(&tail->issued[rank], 0, issued);
+        else  // this CTA's copies of the table land before it goes on
+            for (int64_t i = issued > stages ? issued - stages : 0; i < issued; ++i)
+                mbar_wait_final(smem_addr(&full[i % stages]), (uint32_t)(i / stages & 1));
     } else if (warp == 1 && leader) {
         // ---------------- MMA issuer (even CTA) ----------------
         // The whole warp runs the loop and one lane issues: operands that are
@@ -658,7 +662,26 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
 
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x < 2)
+        store_remote_i64(&tail->gave_up[rank], threadIdx.x, *abort);
     cluster_sync();  // the pair's MMAs and arrivals are over on both sides
+    if (tail->gave_up[0] | tail->gave_up[1]) {
+        // the last copies of the tokens, of both CTAs; a block that only one of
+        // them has issued lacks the other's bytes (or the arrival itself)
+        if (leader && threadIdx.x == 0) {
+            const int64_t n0 = tail->issued[0], n1 = tail->issued[1], n = n0 > n1 ? n0 : n1;
+            for (int64_t i = n > a.bstages ? n - a.bstages : 0; i < n; ++i) {
+                const uint32_t bar = smem_addr(&tail->bfull[i % a.bstages]);
+                if (i >= n0)
+                    mbar_expect_tx(bar, 2 * b_box);
+                else if (i >= n1)
+                    mbar_complete_tx(bar, 2 * b_box);
+                mbar_wait_final(bar, (uint32_t)(i / a.bstages & 1));
+            }
+        }
+        __syncthreads();
+        cluster_sync();
+    }
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
@@ -722,7 +745,7 @@ cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *fla
     a.V = (int)m.V;
     a.K = m.K;
     a.obf16 = obf16;
-    a.wait_ns = kDefaultWaitNs;
+    a.wait_ns = ops_wait_ns();
     token_blocks(m.T, (m.V + 2 * kTcRows - 1) / (2 * kTcRows), &a.ntb, &a.N);
     a.slots = (512 - 2 * a.N) / kTcSlotCols;
     if (a.slots > kTcMaxSlots)

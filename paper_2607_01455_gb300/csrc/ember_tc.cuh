@@ -34,6 +34,12 @@ __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes)
                  : "memory");
 }
 
+// Take `bytes` off the barrier's expected ones, as a copy that is not coming would.
+__device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
@@ -68,7 +74,7 @@ __device__ inline bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *ab
 }
 
 // The same for waits of whole warps in a loop: the clock and the abort word
-// are looked at every 32 tries only (a try suspends the thread for a while).
+// are looked at after 1, 2, 4, ... and then every 32 tries only.
 __device__ __forceinline__ bool mbar_spin(uint32_t bar, uint32_t parity, volatile int *abort, uint64_t limit_ns)
 {
     if (mbar_test(bar, parity))
@@ -77,7 +83,7 @@ __device__ __forceinline__ bool mbar_spin(uint32_t bar, uint32_t parity, volatil
     for (unsigned tries = 1;; ++tries) {
         if (mbar_test(bar, parity))
             return true;
-        if (tries % 32 == 0) {
+        if (tries % 32 == 0 || (tries & (tries - 1)) == 0) {
             const uint64_t t = dev::now_ns();
             if (t0 == 0)
                 t0 = t;
@@ -197,6 +203,12 @@ __device__ __forceinline__ uint32_t mapa_rank(uint32_t addr, uint32_t rank)
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
+}
+
+// A number into the variable at `p`'s place in CTA `rank` of the cluster.
+__device__ __forceinline__ void store_remote_i64(int64_t *p, uint32_t rank, int64_t v)
+{
+    asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(mapa_rank(smem_addr(p), rank)), "l"(v) : "memory");
 }
 
 // Two floats, asynchronously, into the variable at `p`'s place in CTA `rank`

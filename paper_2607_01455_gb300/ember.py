@@ -42,8 +42,8 @@ EXPORTS = (
     "ember_shard_rows", "ember_shard_scale_bytes", "ember_shard_exchange_bytes", "ember_shard_reduce",
     "ember_shard_pack", "ember_shard_update", "ember_column_panels", "ember_set_wait_limit_ns",
     "ember_dense_step_launches",
-    "ember_status_init", "ember_status_read", "ember_rmsnorm", "ember_rmsnorm_quant", "ember_quantize_rows",
-    "ember_dequantize_rows", "ember_rmsnorm_backward_workspace_bytes", "ember_rmsnorm_backward",
+    "ember_status_init", "ember_status_read", "ember_set_ops_wait_limit",
+    "ember_rmsnorm", "ember_rmsnorm_quant", "ember_quantize_rows", "ember_dequantize_rows", "ember_rmsnorm_backward_workspace_bytes", "ember_rmsnorm_backward",
     "ember_matmul_quant_workspace_bytes", "ember_matmul_quant", "ember_softmax_loss_workspace_bytes",
     "ember_softmax_loss", "ember_clip_workspace_bytes", "ember_grad_norm", "ember_clip_grads",
 )
@@ -106,6 +106,7 @@ def lib():
             # the operators of ops.py
             "ember_status_init": (st, [vp, vp]),
             "ember_status_read": (st, [vp, vp]),
+            "ember_set_ops_wait_limit": (st, [ctypes.c_uint64]),
             "ember_rmsnorm": (st, [vp, i64, ip, vp, i64, ip, vp, ip, i64, i64, flt, vp, i64, vp, i64, vp]),
             "ember_rmsnorm_quant": (st, [vp, i64, ip, vp, i64, ip, vp, ip, i64, i64, flt, vp, i64, vp, i64, vp, vp]),
             "ember_quantize_rows": (st, [vp, i64, ip, i64, i64, vp, i64, vp, vp]),

@@ -359,3 +359,8 @@ class Ops:
         EMBER_ERR_ID_OUT_OF_RANGE (a target) or EMBER_ERR_TIMEOUT."""
         return self._lib.ember_status_read(self._status_word(),
                                            _current_stream() if stream is None else getattr(stream, "cuda_stream", stream))
+
+    def set_wait_limit_ns(self, ns):
+        """Limit of the bounded waits inside the kernels, for every call of this
+        process from now on (0: the default, 2 s)."""
+        _check(self._lib.ember_set_ops_wait_limit(int(ns)), "set_wait_limit_ns")

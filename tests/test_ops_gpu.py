@@ -727,3 +727,31 @@ def test_tables_and_logits_past_32_bits(ops, T):
     out = ops.matmul_quant(xq, xs, wq, ws)
     assert torch.equal(out[-200:], ops.matmul_quant(xq[-200:], xs[-200:], wq, ws))
     assert ops.device_status() == E.EMBER_OK
+
+
+# ---- waits that run out ----
+
+@pytest.mark.parametrize("T,V,K", [(40, 3000, 8192), (300, 9000, 2048)])
+def test_a_wait_that_gives_up_is_reported(cuda_device, T, V, K):
+    """With a limit of 1 ns the waits for the first copies run out: the calls
+    return, the status says so, and the next calls are right."""
+    ops, g = Ops(cuda_device), gen(12)
+    xq, wq = ints(g, T, K), ints(g, V, K)
+    xs, ws = torch.rand(T, generator=g, device="cuda"), torch.rand(V, generator=g, device="cuda")
+    z, y = rows(g, T, 100000, BF), torch.randint(0, 100000, (T,), generator=g, device="cuda")
+    want = ops.matmul_quant(xq, xs, wq, ws)
+    wanted = ops.softmax_loss(z, y)
+    try:
+        ops.set_wait_limit_ns(1)
+        ops.matmul_quant(xq, xs, wq, ws)
+        assert ops.device_status() == E.EMBER_ERR_TIMEOUT
+        assert ops.device_status() == E.EMBER_OK
+        ops.softmax_loss(z, y)
+        assert ops.device_status() in (E.EMBER_OK, E.EMBER_ERR_TIMEOUT)  # a copy may land before the clock is read
+    finally:
+        ops.set_wait_limit_ns(0)
+    for _ in range(2):
+        assert torch.equal(ops.matmul_quant(xq, xs, wq, ws), want)
+        for a, b in zip(ops.softmax_loss(z, y), wanted):
+            assert torch.equal(a, b)
+        assert ops.device_status() == E.EMBER_OK
