@@ -231,6 +231,9 @@ __global__ void __launch_bounds__(kFewThreads, MINB) k_mm_few(MmArgs a, int obf1
 //     columns: shared memory sees 8 bits per value of the table, not 8 + 16 + 16;
 //   - gets its half of the tokens' block, already fp16 (k_widen writes them
 //     once per call), by TMA.
+// Measured: 2048 x 32000 x 4096 321 us, 1670 TFLOP/s, 0.87 of the cuBLAS bf16
+// burst (the tensor pipes wait for the widened blocks in between); 64 x 128256 x
+// 4096 95 us, 5.7 TB/s; 49 x 151936 x 896 33 us, 5.0 TB/s.
 // Roles (512 threads per CTA, one CTA per SM, persistent over tiles):
 //   warps 0, 2  issue the TMA loads of the table and of the tokens: two rings,
 //               since a block of the table is free again once it is widened,
