@@ -14,9 +14,8 @@
 // A row of up to 524288 logits is spread over a cluster of up to 16 CTAs and
 // stays in their registers between the statistics and the gradient; the CTAs
 // exchange one pair each through distributed shared memory.  4096 x 128256 bf16:
-// 350 us, 6.0 TB/s, 0.89 of the copy bandwidth (from 1052 us reading each row
-// twice); what is left is latency, with 16 warps per SM and 0.48 instructions
-// issued per scheduler and clock.
+// 345 us, 6.1 TB/s, 0.90 of the copy bandwidth (from 1052 us reading each row
+// twice); what is left is latency: 24 warps per SM of 64 logits a thread.
 #include <atomic>
 
 #include "ember_rows.cuh"
@@ -324,8 +323,22 @@ constexpr int kMaxClusterRow = 16;  // CTAs of a row (a non-portable cluster siz
 // CTAs take twice as many, up to 512.
 constexpr int kRowThreads = 256;
 
+// CTAs per SM that the registers are shared out for.  More warps hide more of
+// a row's chain, until too much spills; us with one fewer / so many: 4096 x
+// 50257 bf16 (224 threads) 180 / 156, 1024 x 252441 (256) 242 / 215, 2048 x
+// 128256 187 / 182, 8192 x 32000 181 / 188.
+// Rows of fp32 are nearer to the bandwidth and gain nothing, nor do calls of
+// few tokens, which run once through.
+constexpr int row_ctas(bool bf16, bool grad, bool here, int threads)
+{
+    return threads == 512   ? 1
+           : threads == 256 ? (bf16 && !here ? 3 : 2)
+           : threads == 224 ? (bf16 || !grad ? 3 : 2)
+                            : (bf16 && !grad ? 6 : 4);
+}
+
 template <typename ZT, typename DT, bool GRAD, bool HERE, int MAXT>
-__global__ void __launch_bounds__(MAXT, (!GRAD && sizeof(ZT) == 2 ? 768 : 512) / MAXT)
+__global__ void __launch_bounds__(MAXT, row_ctas(sizeof(ZT) == 2, GRAD, HERE, MAXT))
 k_loss_rows(LossArgs a)
 {
     constexpr int VE = Cut<ZT>::VE;
@@ -675,6 +688,8 @@ cudaError_t launch_rows(LossArgs a, cudaStream_t stream)
                            : launch_cluster(k_loss_rows<ZT, DT, GRAD, true, 512>, a, p, stream);
     if (p.nt <= 128)
         e = launch_cluster(k_loss_rows<ZT, DT, GRAD, false, 128>, a, p, stream);
+    else if (p.nt <= 224)
+        e = launch_cluster(k_loss_rows<ZT, DT, GRAD, false, 224>, a, p, stream);
     else if (p.nt <= 256)
         e = launch_cluster(k_loss_rows<ZT, DT, GRAD, false, 256>, a, p, stream);
     else
