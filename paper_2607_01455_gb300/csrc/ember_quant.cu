@@ -281,6 +281,8 @@ struct TcArgs {
     int64_t ldo;
     int T, V, K;
     int N, ntb, wstages, bstages, slots, obf16;
+    int split;    // parts of K; with more than one, each writes its sums to
+    float *part;  // part[split][T][V]
     uint32_t idesc;
     uint64_t wait_ns;
 };
@@ -392,6 +394,8 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// SPLIT: the calls whose K is in parts; the others divide by nothing per tile.
+template <bool SPLIT>
 __global__ void __launch_bounds__(kTcThreads, 1)
 k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const TcArgs a)
 {
@@ -407,8 +411,11 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
     const int lane = threadIdx.x & 31;
     const int rank = (int)cluster_rank();
     const bool leader = rank == 0;
-    const int ntiles = (a.V + 2 * kTcRows - 1) / (2 * kTcRows) * a.ntb;
+    const int split = SPLIT ? a.split : 1;
+    const int ntiles = (a.V + 2 * kTcRows - 1) / (2 * kTcRows) * a.ntb * split;  // tiles times parts of K
     const int kblocks = (a.K + kTcK - 1) / kTcK;
+    auto first_block = [&](int tile) { return (int)((int64_t)(tile % split) * kblocks / split); };
+    auto end_block = [&](int tile) { return (int)((int64_t)(tile % split + 1) * kblocks / split); };
     const int tile0 = (int)cluster_id(), tstep = (int)cluster_count();
 
     if (threadIdx.x == 0) {
@@ -463,9 +470,10 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
         const uint64_t pol = l2_policy(tokens ? 1 : a.ntb > 1 ? 0 : 2);
         bool ok = true;
         for (int tile = tile0; tile < ntiles && ok; tile += tstep) {
-            const int vrow = (tile / a.ntb * 2 + rank) * kTcRows;
-            const int trow = tile % a.ntb * a.N + rank * (a.N / 2);
-            for (int kb = 0; kb < kblocks; ++kb) {
+            const int vrow = (tile / split / a.ntb * 2 + rank) * kTcRows;
+            const int trow = tile / split % a.ntb * a.N + rank * (a.N / 2);
+            const int kb1 = end_block(tile);
+            for (int kb = first_block(tile); kb < kb1; ++kb) {
                 if (!mbar_spin(smem_addr(&empty[stage]), phase ^ 1u, abort, a.wait_ns)) {
                     ok = false;
                     break;
@@ -514,7 +522,8 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
                 break;
             }
             const uint32_t d_tmem = tmem + (uint32_t)(acc * a.N);
-            for (int kb = 0; kb < kblocks && ok; ++kb) {
+            const int kb0 = first_block(tile), kb1 = end_block(tile);
+            for (int kb = kb0; kb < kb1 && ok; ++kb) {
                 ok = mbar_spin(full0 + stage * 8, phase, abort, a.wait_ns) &&
                      mbar_spin(afull0 + slot * 8, aphase, abort, a.wait_ns);
                 ok = __all_sync(0xffffffffu, ok);
@@ -527,7 +536,7 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
 #pragma unroll
                     for (int k = 0; k < kTcK / 16; ++k)
                         mma_f16_ta(d_tmem, a_base + k * 8, b_desc + (uint64_t)((k >> 2) * (b_box >> 4) + 2 * (k & 3)),
-                                   a.idesc, (kb | k) != 0);
+                                   a.idesc, ((kb - kb0) | k) != 0);
                     mma_commit_mc(smem_addr(&tail->aempty[slot]));
                 }
                 __syncwarp();
@@ -570,7 +579,7 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
         int seen = -a.slots, bstage = 0;
         bool ok = true;
         for (int tile = tile0; tile < ntiles && ok; tile += tstep) {
-            for (int kb = 0; kb < kblocks; ++kb) {
+            for (int kb = first_block(tile), kb1 = end_block(tile); kb < kb1; ++kb) {
                 ok = mbar_spin(smem_addr(&tail->wfull[stage]), phase, abort, a.wait_ns);
                 if (!__all_sync(0xffffffffu, ok)) {
                     ok = false;
@@ -637,17 +646,20 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
                 break;
             }
             tc_fence_after();
-            const int v = (tile / a.ntb * 2 + rank) * kTcRows + q * 32 + lane;
-            const int t0 = tile % a.ntb * a.N;
-            const float ws = v < a.V ? a.ws[v] : 0.f;
+            const int v = (tile / split / a.ntb * 2 + rank) * kTcRows + q * 32 + lane;
+            const int t0 = tile / split % a.ntb * a.N;
+            const bool whole = split == 1;
+            const float ws = !whole ? 1.f : v < a.V ? a.ws[v] : 0.f;
             const int nt = a.T - t0 < a.N ? a.T - t0 : a.N;  // tokens of this tile
             float *xs = tail->xs[q];
             for (int k = lane; k < a.N; k += 32)
-                xs[k] = k < nt ? a.xs[t0 + k] : 0.f;
+                xs[k] = !whole ? 1.f : k < nt ? a.xs[t0 + k] : 0.f;
             __syncwarp();
             const uint32_t d_tmem = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * a.N);
             const int64_t at = (int64_t)t0 * a.ldo + v;
-            if (a.obf16)
+            if (!whole)
+                write_tile(a.part + ((int64_t)(tile % split) * a.T + t0) * a.V + v, a.V, d_tmem, xs, ws, nt, v < a.V);
+            else if (a.obf16)
                 write_tile(static_cast<unsigned short *>(a.out) + at, a.ldo, d_tmem, xs, ws, nt, v < a.V);
             else
                 write_tile(static_cast<float *>(a.out) + at, a.ldo, d_tmem, xs, ws, nt, v < a.V);
@@ -692,6 +704,22 @@ k_mm_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtens
     }
 }
 
+// The parts of K joined, in order, and scaled.
+__global__ void __launch_bounds__(256) k_mm_join(const TcArgs a)
+{
+    const int v = blockIdx.x * 256 + threadIdx.x;
+    const int64_t t = blockIdx.y;
+    dev::grid_dep_wait();
+    dev::grid_dep_launch();
+    if (v >= a.V)
+        return;
+    float s = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < a.split; ++k)
+        s += a.part[((int64_t)k * a.T + t) * a.V + v];
+    store_out(a.out, a.obf16, t * a.ldo + v, s * a.xs[t] * a.ws[v]);
+}
+
 // R x C elements of `size` bytes with a row stride of ld, boxes of 128 bytes x
 // `rows` in the 128-byte swizzle; what lies outside reads as zero.
 bool make_load_map(CUtensorMap *m, const void *base, int size, int64_t C, int64_t R, int64_t ld, int rows)
@@ -731,6 +759,30 @@ void token_blocks(int64_t T, int64_t vblocks, int *ntb, int *N)
 
 int64_t widened_cols(int64_t K) { return (K + 7) / 8 * 8; }
 
+// Plan of a call on the tensor cores.  Where the tiles leave half of the SM
+// pairs or more without one, K is split among them, 8 blocks or more to a
+// part, if that takes 12 blocks or more off every pair (about what the joining
+// launch costs); us whole / in parts: 64 x 4161 x 7856 30 / 17 (4 parts), 20 x
+// 1000 x 4096 17.8 / 13.0 (4), 64 x 9000 x 2048 12.9 / 14.4 (2, not taken).
+struct TcPlan {
+    int ntb, N, split;
+    size_t part_at, bytes;  // where the parts begin in the workspace, and its size
+};
+TcPlan tc_plan(int64_t T, int64_t V, int64_t K)
+{
+    TcPlan p;
+    const int64_t vblocks = (V + 2 * kTcRows - 1) / (2 * kTcRows), kblocks = (K + kTcK - 1) / kTcK;
+    token_blocks(T, vblocks, &p.ntb, &p.N);
+    const int64_t tiles = vblocks * p.ntb;
+    const int64_t by_pairs = kSms / 2 / tiles, by_blocks = kblocks / 8;
+    p.split = (int)(by_pairs < by_blocks ? by_pairs : by_blocks);
+    if (p.split < 2 || kblocks - (kblocks + p.split - 1) / p.split < 12)
+        p.split = 1;
+    p.part_at = ((size_t)(T * widened_cols(K)) * 2 + 255) / 256 * 256;
+    p.bytes = p.part_at + (p.split > 1 ? (size_t)p.split * T * V * sizeof(float) : 0);
+    return p;
+}
+
 cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *flags, cudaStream_t stream)
 {
     const int kp = (int)widened_cols(m.K);
@@ -749,7 +801,11 @@ cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *fla
     a.K = m.K;
     a.obf16 = obf16;
     a.wait_ns = ops_wait_ns();
-    token_blocks(m.T, (m.V + 2 * kTcRows - 1) / (2 * kTcRows), &a.ntb, &a.N);
+    const TcPlan p = tc_plan(m.T, m.V, m.K);
+    a.ntb = p.ntb;
+    a.N = p.N;
+    a.split = p.split;
+    a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + p.part_at);
     a.slots = (512 - 2 * a.N) / kTcSlotCols;
     if (a.slots > kTcMaxSlots)
         a.slots = kTcMaxSlots;
@@ -765,7 +821,8 @@ cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *fla
     if (!make_load_map(&tm_w, m.wq, 1, m.K, m.V, m.ldw, kTcRows) ||
         !make_load_map(&tm_x, workspace, 2, kp, m.T, kp, a.N / 2))
         return cudaErrorInvalidValue;
-    e = cudaFuncSetAttribute(k_mm_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTcSmem);
+    const auto kernel = a.split > 1 ? k_mm_tc<true> : k_mm_tc<false>;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTcSmem);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
@@ -781,16 +838,19 @@ cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *fla
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    const int64_t tiles = (m.V + 2 * kTcRows - 1) / (2 * kTcRows) * a.ntb;
+    const int64_t tiles = (m.V + 2 * kTcRows - 1) / (2 * kTcRows) * a.ntb * a.split;
     cfg.gridDim = dim3(kSms);
     int fit = 0;
-    e = cudaOccupancyMaxActiveClusters(&fit, k_mm_tc, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg);
     if (e != cudaSuccess)
         return e;
     if (fit < 1)
         return cudaErrorInvalidConfiguration;
     cfg.gridDim = dim3((unsigned)(2 * (tiles < fit ? tiles : fit)));
-    return cudaLaunchKernelEx(&cfg, k_mm_tc, tm_w, tm_x, a);
+    e = cudaLaunchKernelEx(&cfg, kernel, tm_w, tm_x, a);
+    if (e == cudaSuccess && a.split > 1)
+        e = launch_k(k_mm_join, dim3((unsigned)((m.V + 255) / 256), (unsigned)m.T), dim3(256), 0, stream, true, a);
+    return e;
 }
 
 template <int TN, int R, int MINB, int UNR>
@@ -848,7 +908,7 @@ size_t ember_matmul_quant_workspace_bytes(int64_t T, int64_t V, int64_t K)
 {
     if (T < 0 || V < 1 || K < 1 || T > kMaxMmRows || V > kMaxMmRows || K > kMaxRowCols)
         return 0;
-    return (size_t)(T * widened_cols(K)) * 2 + 256;  // the tokens in fp16
+    return tc_plan(T > 0 ? T : 1, V, K).bytes;  // the tokens in fp16, the parts of a split K
 }
 
 ember_status ember_matmul_quant(const int8_t *xq, int64_t ldx, const float *xs, const int8_t *wq, int64_t ldw,

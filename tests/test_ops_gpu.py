@@ -286,7 +286,8 @@ MM_SHAPES = [(1, 1, 1), (1, 5, 3), (1, 1000, 64), (1, 3001, 896), (1, 129, 8192)
              (4, 1000, 112), (7, 511, 1003), (8, 2000, 2048), (8, 100, 32768), (9, 300, 64), (16, 256, 128),
              (17, 255, 144), (31, 1030, 896), (49, 5000, 896), (64, 512, 1000), (65, 700, 200), (127, 129, 272),
              (128, 1280, 512), (200, 1000, 4096), (257, 515, 1008), (400, 900, 65), (1000, 2049, 320), (33, 40, 8192),
-             (12, 70000, 96), (0, 64, 64), (6, 20000, 256), (3, 17000, 2064), (2, 30, 20000)]
+             (12, 70000, 96), (0, 64, 64), (6, 20000, 256), (3, 17000, 2064), (2, 30, 20000),
+             (64, 4161, 7856), (10, 500, 4099), (190, 300, 2048), (129, 255, 32768), (500, 1100, 3000)]
 
 
 @pytest.mark.parametrize("T,V,K", MM_SHAPES)
