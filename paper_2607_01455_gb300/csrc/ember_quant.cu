@@ -873,10 +873,11 @@ cudaError_t launch_few(const MmArgs &a, int obf16, int kpad, cudaStream_t stream
 //   4 rows, 4 CTAs, 4 slabs   24 /  - /  -    162 /   - /   -
 //   8 rows, 2 CTAs, 4 slabs   25 / 29 /  -    158 / 166 /   -
 //   k_mm_tc                   31 / 31 / 31    179 / 179 / 180
-// Five to eight tokens go to the tensor cores where the table has a tile for
-// most SM pairs (4161 x 7856, 17 tiles: 17 us here, 30 there).
+// Five to eight tokens go to the tensor cores for large tables (k_mm_few / k_mm_tc
+// for 6 tokens: 10000 x 2048 9.0 / 12.6, 40000 x 8192 75 / 81, 50257 x 768 16.6 /
+// 13.7).
 constexpr int kFewShortRow = 2048;
-constexpr int64_t kFewMaxRows = 16384;
+constexpr int64_t kFewMaxRows = 49152;
 
 cudaError_t launch_mm(const MmArgs &a, int obf16, void *workspace, unsigned *flags, cudaStream_t stream)
 {
