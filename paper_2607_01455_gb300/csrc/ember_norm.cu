@@ -20,8 +20,9 @@
 // Measured, of the copy bandwidth (6780 GB/s): norm 8192 x 4096 bf16 with an
 // fp32 residual 60.7 us, 0.98; 8192 x 8192 bf16 with residual 79 us, 1.00;
 // in 8 bits 76 us, 0.91; backward with dres 89 us, 0.89 (fp32 156 us, 1.02).
-// Rows off the 16-byte boundaries read and write single elements: 16384 x 1003
-// bf16 59 us, 0.33.
+// Rows off the 16-byte boundaries: 0.2 to 0.85 (k_rmsnorm_shifted).
+#include <type_traits>
+
 #include "ember_rows.cuh"
 
 namespace ember {
@@ -443,6 +444,215 @@ cudaError_t launch_ring(K kernel, const A &a, const RingPlan &p, int64_t grid, c
     return launch_k(kernel, dim3((unsigned)grid), dim3(p.block), p.smem, stream, true, a);
 }
 
+// Rows off the 16-byte boundaries, one per CTA at a time.  In memory they are
+// taken in the 16-byte units of their addresses, through shared memory where
+// they keep their shift, with single elements at both ends; between, a thread
+// has columns tid, tid + nt, ... of every row, whatever the shifts of the
+// arrays.  The units come asynchronously, two rows ahead, the single elements
+// in a register, one row ahead.  bf16, us, element by element from memory / so:
+// x + residual 16384 x 1003 59 / 37, 8192 x 4095 185 / 62; in 8 bits (x alone)
+// 69 / 39, 221 / 76; backward 76 / 48, 197 / 89.  Columns per thread: 16 from 512
+// columns on (8192 x 4095 x + residual 62 us, 82 with 8), 8 for shorter rows
+// (65536 x 130 41 us, 47 with 16) and for 8 bits, whose second reduction wants
+// the warps (76 us, 92 with 16).
+template <typename T>
+struct RowCut {
+    static constexpr int VE = 16 / sizeof(T);
+    int shift, head, units, tail;
+    __device__ __forceinline__ RowCut(const T *p, int D)
+    {
+        shift = (int)((uintptr_t)p & 15);
+        head = shift ? (16 - shift) / (int)sizeof(T) : 0;
+        head = head < D ? head : D;
+        units = (D - head) / VE;
+        tail = D - head - units * VE;
+    }
+    // The single element of this thread, or -1.
+    __device__ __forceinline__ int edge(int D) const
+    {
+        const int t = threadIdx.x;
+        return t < head ? t : t < head + tail ? D - tail + (t - head) : -1;
+    }
+    __device__ __forceinline__ int at(int col) const { return shift + col * (int)sizeof(T); }
+};
+template <typename T>
+__host__ __device__ constexpr int shifted_bytes(int D)
+{
+    return (D * (int)sizeof(T) + 15) / 16 * 16 + 16;
+}
+template <typename T>
+__device__ __forceinline__ void shifted_fetch(unsigned char *to, const T *row, int D)
+{
+    const RowCut<T> c(row, D);
+    for (int u = threadIdx.x; u < c.units; u += blockDim.x)
+        copy16(to + c.at(c.head) + u * 16, row + c.head + u * RowCut<T>::VE);
+}
+template <typename T>
+__device__ __forceinline__ T shifted_edge(const T *row, int D, bool on)
+{
+    const int e = on ? RowCut<T>(row, D).edge(D) : -1;
+    return e >= 0 ? row[e] : T{};
+}
+template <typename T>
+__device__ __forceinline__ void shifted_put_edge(unsigned char *to, const T *row, int D, T v)
+{
+    const RowCut<T> c(row, D);
+    const int e = c.edge(D);
+    if (e >= 0)
+        *reinterpret_cast<T *>(to + c.at(e)) = v;
+}
+__device__ __forceinline__ float as_float(float v) { return v; }
+__device__ __forceinline__ float as_float(bf16_t v) { return __uint_as_float((unsigned)v.u << 16); }
+__device__ __forceinline__ void from_float(float &o, float v) { o = v; }
+__device__ __forceinline__ void from_float(bf16_t &o, float v) { o.u = dev::f2bf(v); }
+// A finished row from shared memory to where it belongs.
+template <typename T>
+__device__ __forceinline__ void shifted_store(T *row, const unsigned char *from, int D)
+{
+    const RowCut<T> c(row, D);
+    for (int u = threadIdx.x; u < c.units; u += blockDim.x)
+        *reinterpret_cast<uint4 *>(row + c.head + u * RowCut<T>::VE) =
+            *reinterpret_cast<const uint4 *>(from + c.at(c.head) + u * 16);
+    const int e = c.edge(D);
+    if (e >= 0)
+        row[e] = *reinterpret_cast<const T *>(from + c.at(e));
+}
+
+template <typename XT, typename RT, bool RES, bool NORM, int OUT, int NV>
+__global__ void __launch_bounds__(NV == 16 ? 512 : 1024, 1) k_rmsnorm_shifted(NormArgs a)
+{
+    using YT = std::conditional_t<OUT == kOutInt, int8_t, XT>;
+    extern __shared__ __align__(128) unsigned char sm[];  // [stage][x, residual], h, y
+    __shared__ float part[2][2][32];
+    const int tid = threadIdx.x, nt = blockDim.x, D = a.D;
+    const int x_bytes = shifted_bytes<XT>(D), stage_bytes = x_bytes + (RES ? shifted_bytes<RT>(D) : 0);
+    unsigned char *hbuf = sm + kRing * stage_bytes, *ybuf = hbuf + (RES ? shifted_bytes<RT>(D) : 0);
+    const XT *x = static_cast<const XT *>(a.x);
+    const RT *res = static_cast<const RT *>(a.res);
+    dev::grid_dep_wait();
+    dev::grid_dep_launch();
+    auto fetch = [&](int64_t row, int stage) {
+        if (row < a.T) {
+            shifted_fetch<XT>(sm + stage * stage_bytes, x + row * a.ldx, D);
+            if constexpr (RES)
+                shifted_fetch<RT>(sm + stage * stage_bytes + x_bytes, res + row * a.ldr, D);
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kRing; ++s)
+        fetch(blockIdx.x + (int64_t)s * gridDim.x, s);
+    XT xe = shifted_edge<XT>(x + blockIdx.x * a.ldx, D, true);
+    RT re{};
+    if constexpr (RES)
+        re = shifted_edge<RT>(res + blockIdx.x * a.ldr, D, true);
+    float g[NV];
+    if constexpr (NORM) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float one[1] = {0.f};
+            if (k * nt + tid < D)
+                load_gain<1>(a.gain, a.gbf16, k * nt + tid, one);
+            g[k] = one[0];
+        }
+    }
+    int stage = 0, par = 0;
+    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, par ^= 1) {
+        unsigned char *xb = sm + stage * stage_bytes, *rb = xb + x_bytes;
+        const XT *xr = x + row * a.ldx;
+        const RT *rr = RES ? res + row * a.ldr : nullptr;
+        copies_wait<kRing - 1>();
+        shifted_put_edge<XT>(xb, xr, D, xe);
+        const bool more = row + gridDim.x < a.T;
+        xe = shifted_edge<XT>(xr + (int64_t)gridDim.x * a.ldx, D, more);
+        if constexpr (RES) {
+            shifted_put_edge<RT>(rb, rr, D, re);
+            re = shifted_edge<RT>(rr + (int64_t)gridDim.x * a.ldr, D, more);
+        }
+        __syncthreads();
+        RT *hrow = RES ? static_cast<RT *>(a.h) + row * a.ldh : nullptr;
+        YT *yrow = static_cast<YT *>(a.y) + row * a.ldy;
+        const int xs = (int)((uintptr_t)xr & 15), rs = (int)((uintptr_t)rr & 15), hs = (int)((uintptr_t)hrow & 15),
+                  ys = (int)((uintptr_t)yrow & 15);
+        float s[NV];
+        float ss = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int j = k * nt + tid;
+            s[k] = 0.f;
+            if (j < D) {
+                s[k] = as_float(reinterpret_cast<const XT *>(xb + xs)[j]);
+                if constexpr (RES) {
+                    s[k] += as_float(reinterpret_cast<const RT *>(rb + rs)[j]);
+                    from_float(reinterpret_cast<RT *>(hbuf + hs)[j], s[k]);
+                }
+                ss = fmaf(s[k], s[k], ss);
+            }
+        }
+        if constexpr (NORM) {
+            const float rstd = 1.f / sqrtf(cta_join<false>(ss, part[par][0]) / (float)D + a.eps);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                s[k] = s[k] * rstd * g[k];
+        }
+        if constexpr (OUT == kOutInt) {
+            float top = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                top = max_nan(top, fabsf(s[k]));
+            const RowScale sc = row_scale(cta_join<true>(top, part[par][1]));
+            const bool zero = !sc.divide && sc.inv == 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (k * nt + tid < D)
+                    reinterpret_cast<int8_t *>(ybuf + ys)[k * nt + tid] = zero ? 0 : (int8_t)(quant(s[k], sc) & 0xff);
+            if (tid == 0)
+                a.scales[row] = sc.scale;
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (k * nt + tid < D)
+                    from_float(reinterpret_cast<XT *>(ybuf + ys)[k * nt + tid], s[k]);
+        }
+        __syncthreads();  // the outputs are whole, and every thread has read its inputs
+        fetch(row + (int64_t)kRing * gridDim.x, stage);
+        stage = stage + 1 == kRing ? 0 : stage + 1;
+        if constexpr (RES)
+            shifted_store<RT>(hrow, hbuf, D);
+        shifted_store<YT>(yrow, ybuf, D);
+    }
+    copies_wait<0>();
+}
+
+// Columns per thread, threads, CTAs and shared memory of the kernels for
+// shifted rows.
+struct ShiftPlan {
+    bool on;
+    int cols, block, per_sm;
+    size_t smem;
+};
+ShiftPlan shift_plan(int64_t D, size_t stage_bytes, size_t out_bytes, bool wide)
+{
+    ShiftPlan p{};
+    p.cols = wide && D >= 512 ? 16 : 8;
+    p.block = round32((int)((D + p.cols - 1) / p.cols));
+    p.smem = kRing * stage_bytes + out_bytes;
+    p.on = D <= 8192 && p.smem <= 200 << 10;
+    p.per_sm = (int)((220 << 10) / (p.smem + 2048));
+    const int by_regs = (p.cols == 16 ? 768 : 1024) / p.block;
+    p.per_sm = p.per_sm < by_regs ? p.per_sm : by_regs;
+    p.per_sm = p.per_sm > 32 ? 32 : p.per_sm < 1 ? 1 : p.per_sm;
+    return p;
+}
+template <typename K, typename A>
+cudaError_t launch_shifted(K kernel, const A &a, const ShiftPlan &p, int64_t grid, cudaStream_t stream)
+{
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10);
+    if (e != cudaSuccess)
+        return e;
+    return launch_k(kernel, dim3((unsigned)grid), dim3(p.block), p.smem, stream, true, a);
+}
+
 // Groups per thread: one while the rows alone do not fill the GPU (a call of
 // a few tokens is all latency), four otherwise: two or eight were 10 to 60 %
 // slower on 65536 x 1024 to 8192 x 8192.  Rows off the 16-byte boundaries are
@@ -473,9 +683,17 @@ cudaError_t pick_norm(const NormArgs &a, bool grouped8, cudaStream_t stream)
         }
         return go_norm<XT, RT, RES, NORM, OUT, 8, 4>(a, stream);
     }
-    if (a.D <= 4096)
-        return go_norm<XT, RT, RES, NORM, OUT, 1, 4>(a, stream);
-    return go_norm<XT, RT, RES, NORM, OUT, 1, 32>(a, stream);
+    using YT = std::conditional_t<OUT == kOutInt, int8_t, XT>;
+    const size_t r = RES ? shifted_bytes<RT>(a.D) : 0;
+    const ShiftPlan p = shift_plan(a.D, shifted_bytes<XT>(a.D) + r, r + shifted_bytes<YT>(a.D), OUT == kOutSame);
+    if (!p.on)
+        return go_norm<XT, RT, RES, NORM, OUT, 1, 32>(a, stream);
+    const int64_t most = (int64_t)kSms * p.per_sm, grid = a.T < most ? a.T : most;
+    if constexpr (OUT == kOutSame) {
+        if (p.cols == 16)
+            return launch_shifted(k_rmsnorm_shifted<XT, RT, RES, NORM, OUT, 16>, a, p, grid, stream);
+    }
+    return launch_shifted(k_rmsnorm_shifted<XT, RT, RES, NORM, OUT, 8>, a, p, grid, stream);
 }
 
 template <int OUT>
@@ -707,6 +925,109 @@ __global__ void __launch_bounds__(MAXT, MINB) k_rmsnorm_back_ring(BackArgs a)
     }
 }
 
+// The same for rows off the 16-byte boundaries, as k_rmsnorm_shifted takes them.
+template <typename XT, bool RES, int NV>
+__global__ void __launch_bounds__(NV == 16 ? 512 : 1024, 1) k_rmsnorm_back_shifted(BackArgs a)
+{
+    constexpr int NIN = RES ? 3 : 2;
+    extern __shared__ __align__(128) unsigned char sm[];  // [stage][dy, h, dres], dx
+    __shared__ float part[2][2][32];
+    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, w = tid >> 5, nw = nt >> 5, D = a.D;
+    const int row_bytes = shifted_bytes<XT>(D), stage_bytes = NIN * row_bytes;
+    unsigned char *obuf = sm + kRing * stage_bytes;
+    const XT *in[3] = {static_cast<const XT *>(a.dy), static_cast<const XT *>(a.h), static_cast<const XT *>(a.dres)};
+    const int64_t ld[3] = {a.lddy, a.ldh, a.lddres};
+    dev::grid_dep_wait();
+    dev::grid_dep_launch();
+    auto fetch = [&](int64_t row, int stage) {
+        if (row < a.T) {
+#pragma unroll
+            for (int i = 0; i < NIN; ++i)
+                shifted_fetch<XT>(sm + stage * stage_bytes + i * row_bytes, in[i] + row * ld[i], D);
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kRing; ++s)
+        fetch(blockIdx.x + (int64_t)s * gridDim.x, s);
+    XT edge[NIN];
+#pragma unroll
+    for (int i = 0; i < NIN; ++i)
+        edge[i] = shifted_edge<XT>(in[i] + blockIdx.x * ld[i], D, true);
+    float g[NV], acc[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        float one[1] = {0.f};
+        if (k * nt + tid < D)
+            load_gain<1>(a.gain, a.gbf16, k * nt + tid, one);
+        g[k] = one[0];
+        acc[k] = 0.f;
+    }
+    const float inv_D = 1.f / (float)D;
+    int stage = 0, par = 0;
+    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, par ^= 1) {
+        copies_wait<kRing - 1>();
+        const bool more = row + gridDim.x < a.T;
+        const unsigned char *from[NIN];
+#pragma unroll
+        for (int i = 0; i < NIN; ++i) {
+            unsigned char *b = sm + stage * stage_bytes + i * row_bytes;
+            const XT *r = in[i] + row * ld[i];
+            shifted_put_edge<XT>(b, r, D, edge[i]);
+            edge[i] = shifted_edge<XT>(r + (int64_t)gridDim.x * ld[i], D, more);
+            from[i] = b + ((uintptr_t)r & 15);
+        }
+        __syncthreads();
+        float fy[NV], fh[NV], fr[NV];
+        float ss = 0.f, dot = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int j = k * nt + tid;
+            const bool on = j < D;
+            fy[k] = on ? as_float(reinterpret_cast<const XT *>(from[0])[j]) : 0.f;
+            fh[k] = on ? as_float(reinterpret_cast<const XT *>(from[1])[j]) : 0.f;
+            fr[k] = 0.f;
+            if constexpr (RES)
+                fr[k] = on ? as_float(reinterpret_cast<const XT *>(from[2])[j]) : 0.f;
+            ss = fmaf(fh[k], fh[k], ss);
+            dot = fmaf(fy[k] * g[k], fh[k], dot);
+        }
+        ss = warp_sum(ss);
+        dot = warp_sum(dot);
+        if (nw > 1) {
+            if (lane == 0) {
+                part[par][0][w] = ss;
+                part[par][1][w] = dot;
+            }
+            __syncthreads();
+            ss = warp_sum(lane < nw ? part[par][0][lane] : 0.f);
+            dot = warp_sum(lane < nw ? part[par][1][lane] : 0.f);
+        }
+        const float r = 1.f / sqrtf(ss * inv_D + a.eps);
+        const float c = r * r * (dot * inv_D);
+        XT *orow = static_cast<XT *>(a.dx) + row * a.lddx;
+        XT *o = reinterpret_cast<XT *>(obuf + ((uintptr_t)orow & 15));
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int j = k * nt + tid;
+            if (j < D) {
+                from_float(o[j], fmaf(r, fmaf(-fh[k], c, fy[k] * g[k]), fr[k]));
+                acc[k] = fmaf(fy[k], fh[k] * r, acc[k]);
+            }
+        }
+        __syncthreads();
+        fetch(row + (int64_t)kRing * gridDim.x, stage);
+        stage = stage + 1 == kRing ? 0 : stage + 1;
+        shifted_store<XT>(orow, obuf, D);
+    }
+    copies_wait<0>();
+    float *p = a.partial + (int64_t)blockIdx.x * D;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+        if (k * nt + tid < D)
+            p[k * nt + tid] = acc[k];
+}
+
 // dgain_j = the sum of the n partial rows of column j: 32 columns a CTA, each
 // by 32 threads that take every 32nd row, then joined in order.
 __global__ void __launch_bounds__(1024) k_dgain(const float *__restrict__ partial, int n, int D,
@@ -730,24 +1051,30 @@ __global__ void __launch_bounds__(1024) k_dgain(const float *__restrict__ partia
 
 struct BackPlan {
     RingPlan ring;
+    ShiftPlan shift;
     int vec, nv, tpr, block, grid;
     int64_t parts;  // partial rows
 };
 
-// Long rows of whole groups go through the ring; the rest keeps one row in
-// registers.
+// Long rows of whole groups go through the ring, rows off the boundaries through
+// shared memory with their shifts; the rest keeps one row in registers.
 BackPlan back_plan(int64_t T, int64_t D, int esize, bool res, bool grouped8)
 {
     BackPlan p{};
     p.ring = ring_plan(D, (res ? 3 : 2) * D * esize);
     p.ring.on = p.ring.on && grouped8;
+    const size_t row = (size_t)(esize == 2 ? shifted_bytes<bf16_t>((int)D) : shifted_bytes<float>((int)D));
+    p.shift = shift_plan(D, (res ? 3 : 2) * row, row, true);
+    p.shift.on = p.shift.on && !grouped8;
     p.vec = grouped8 ? 8 : 1;
-    p.nv = grouped8 ? (D <= 2048 ? 1 : D <= 8192 ? 2 : 4) : (D <= 4096 ? 4 : 32);
+    p.nv = grouped8 ? (D <= 2048 ? 1 : D <= 8192 ? 2 : 4) : 32;
     p.tpr = threads_per_row(D, p.vec, p.nv);
     p.block = p.tpr < kMinBlock ? kMinBlock : p.tpr;
-    const int64_t rpc = p.ring.on ? 1 : p.block / p.tpr;
+    const int64_t rpc = p.ring.on || p.shift.on ? 1 : p.block / p.tpr;
     const int64_t want = (T + rpc - 1) / rpc;
-    const int64_t most = (int64_t)kSms * (p.ring.on ? p.ring.per_sm : p.block >= 1024 ? 1 : 1024 / p.block);
+    const int64_t most = (int64_t)kSms * (p.ring.on    ? p.ring.per_sm
+                                          : p.shift.on ? p.shift.per_sm
+                                                       : (p.block >= 1024 ? 1 : 1024 / p.block));
     p.grid = (int)(want < most ? want : most);
     p.parts = p.grid * rpc;
     return p;
@@ -760,6 +1087,9 @@ cudaError_t launch_back(BackArgs a, const BackPlan &p, cudaStream_t stream)
     if (p.ring.on)
         return p.ring.block <= 256 ? launch_ring(k_rmsnorm_back_ring<XT, RES, 256, 2>, a, p.ring, p.grid, stream)
                                    : launch_ring(k_rmsnorm_back_ring<XT, RES, 512, 1>, a, p.ring, p.grid, stream);
+    if (p.shift.on)
+        return p.shift.cols == 16 ? launch_shifted(k_rmsnorm_back_shifted<XT, RES, 16>, a, p.shift, p.grid, stream)
+                                  : launch_shifted(k_rmsnorm_back_shifted<XT, RES, 8>, a, p.shift, p.grid, stream);
     auto go = [&](auto kernel) { return launch_k(kernel, dim3(p.grid), dim3(p.block), 0, stream, true, a); };
     if (p.vec == 8) {
         if (p.nv == 1)
@@ -768,8 +1098,6 @@ cudaError_t launch_back(BackArgs a, const BackPlan &p, cudaStream_t stream)
             return go(k_rmsnorm_back<XT, RES, 8, 2, 512>);
         return p.block <= 512 ? go(k_rmsnorm_back<XT, RES, 8, 4, 512>) : go(k_rmsnorm_back<XT, RES, 8, 4, 1024>);
     }
-    if (p.nv == 4)
-        return go(k_rmsnorm_back<XT, RES, 1, 4, 1024>);
     return p.block <= 512 ? go(k_rmsnorm_back<XT, RES, 1, 32, 512>) : go(k_rmsnorm_back<XT, RES, 1, 32, 1024>);
 }
 
