@@ -304,7 +304,7 @@ struct Cut {
     }
 };
 
-// The larger of two units, value by value (a NaN loses; it is found in the sum).
+// The largest value of a unit (a NaN loses; it is found in the sum).
 template <typename ZT>
 __device__ __forceinline__ float unit_max(const uint4 &r)
 {
