@@ -2,11 +2,14 @@
 
 Each .cu file compiles to an object in parallel, then nvcc links the shared
 library in place under paper_2607_01455_gb300/_lib/.  nvcc cross-compiles, so
-this runs on a machine without a GPU too.
+this runs on a machine without a GPU too.  Beside it: the operators' binding
+to torch tensors, host code compiled against the headers of the torch at hand.
 """
 import concurrent.futures
 import os
+import shutil
 import subprocess
+import sysconfig
 import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -16,6 +19,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB_DIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIB_DIR, "libember.so")
+BINDING = os.path.join(LIB_DIR, "_ops_binding.so")
 
 NVCC = os.environ.get("NVCC", "nvcc")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -56,6 +60,28 @@ def build_library(force: bool = False, verbose_ptxas: bool = False) -> str:
     return LIB
 
 
+def build_binding(force: bool = False) -> str:
+    """Build the operators' binding unless it is newer than its source."""
+    src = os.path.join(CSRC, "ops_binding.cpp")
+    if (not force and os.path.exists(BINDING)
+            and os.path.getmtime(BINDING) >= max(os.path.getmtime(p) for p in (src, os.path.join(INCLUDE, "ember.h")))):
+        return BINDING
+    import torch
+    os.makedirs(LIB_DIR, exist_ok=True)
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which(NVCC) or "/usr/local/cuda/bin/nvcc")))
+    dirs = [INCLUDE, sysconfig.get_paths()["include"], os.path.join(home, "include"),
+            os.path.join(home, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
+    libs = os.path.join(home, "lib")
+    tmp = BINDING + f".tmp{os.getpid()}"
+    subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                    *(a for d in dirs for a in ("-I", d)), src, "-o", tmp, "-L", libs, "-lc10", "-lc10_cuda",
+                    "-ltorch_cpu", "-ltorch", "-ltorch_python", f"-Wl,-rpath,{libs}"], check=True)
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 if __name__ == "__main__":
     import sys
     print(build_library(force=True, verbose_ptxas="-v" in sys.argv))
+    print(build_binding(force=True))

@@ -12,6 +12,7 @@ import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_lib", "libember.so")
+BINDING_PATH = os.path.join(_HERE, "_lib", "_ops_binding.so")
 
 EMBER_OK = 0
 EMBER_ERR_INVALID_ARG = 1
@@ -129,6 +130,33 @@ def lib():
             fn.argtypes = args
         _lib = L
     return _lib
+
+
+# What the binding calls, in the order of its table.
+_BOUND = ("ember_rmsnorm", "ember_rmsnorm_quant", "ember_rmsnorm_backward_workspace_bytes", "ember_rmsnorm_backward",
+          "ember_dequantize_rows", "ember_matmul_quant_workspace_bytes", "ember_matmul_quant",
+          "ember_softmax_loss_workspace_bytes", "ember_softmax_loss", "ember_clip_workspace_bytes",
+          "ember_clip_grads", "ember_grad_norm")
+_binding = None
+
+
+def ops_binding():
+    """The compiled calls of the operators on torch tensors, bound to libember;
+    raises if they have not been built."""
+    global _binding
+    if _binding is None:
+        import importlib.util
+
+        import torch  # noqa: F401  (its libraries have to be loaded first)
+        L = lib()
+        if not os.path.exists(BINDING_PATH):
+            raise RuntimeError(f"{BINDING_PATH} is missing: build it with __graft_entry__.build()")
+        spec = importlib.util.spec_from_file_location("_ops_binding", BINDING_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.bind(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in _BOUND))
+        _binding = module
+    return _binding
 
 
 def _addr(x):

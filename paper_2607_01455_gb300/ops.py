@@ -14,7 +14,10 @@ global gradient norm and clipping.
 
 Every computation runs in libember (include/ember.h has each operator's
 definition and limits); this module checks shapes, types and devices, makes
-the outputs that were not passed in, and marshals the arguments.  Matrices
+the outputs that were not passed in, and marshals the arguments.  The common
+calls take a compiled form of the same steps (csrc/ops_binding.cpp) and come
+here only with arguments that it passes on: those that need a larger workspace,
+that have unusual strides, or that are refused.  Matrices
 are 2-D with unit stride along their rows; any row stride is accepted.  Calls
 run on torch's current stream, or on `stream` (a torch stream), whose memory
 their outputs and workspace then come from; a tensor that another stream
@@ -25,7 +28,7 @@ from array import array
 import torch
 
 from .ember import (EMBER_BF16, EMBER_ERR_DTYPE, EMBER_ERR_INVALID_ARG, EMBER_F32, EMBER_I32, EMBER_I64, EMBER_OK,
-                    EmberError, _check, _current_stream, lib)
+                    EmberError, _check, _current_stream, lib, ops_binding)
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
@@ -52,7 +55,9 @@ class Ops:
         self.device = torch.device("cuda", torch.cuda.current_device() if dev.index is None else dev.index)
         self._index = self.device.index
         self._lib = lib()
+        self._fast = ops_binding()
         self._status = self._workspace = None  # made by the first call that needs them, on its stream
+        self._at = self._bytes = 0  # the workspace's address and size
         self._kept = []
         self._sizes = {}  # workspace bytes by operator and sizes
 
@@ -105,6 +110,7 @@ class Ops:
             w = torch.empty(size, dtype=torch.uint8, device=self.device)
             self._kept.append(w)
             self._workspace = w
+            self._at, self._bytes = w.data_ptr(), size
         return w
 
     def _status_word(self):
@@ -138,6 +144,9 @@ class Ops:
             with self._on(stream):
                 return self.rmsnorm(x, gain, residual, eps, out, residual_out)
         w = "rmsnorm"
+        r = self._fast.rmsnorm(self._index, x, gain, residual, eps, out, residual_out)
+        if r is not None:
+            return r if r.__class__ is not int else _check(r, w)
         px, ldx = self._matrix(w, "x", x, _TYPES)
         shape, xt = x.shape, x.dtype
         T, D = shape
@@ -164,6 +173,9 @@ class Ops:
             with self._on(stream):
                 return self.rmsnorm_quant(x, gain, residual, eps, residual_out)
         w = "rmsnorm_quant"
+        r = self._fast.rmsnorm_quant(self._index, x, gain, residual, eps, residual_out)
+        if r is not None:
+            return r if r.__class__ is not int else _check(r, w)
         px, ldx = self._matrix(w, "x", x, _TYPES)
         T, D = x.shape
         pg, gt = self._gain(w, gain, D)
@@ -186,6 +198,9 @@ class Ops:
             with self._on(stream):
                 return self.rmsnorm_backward(dy, h, gain, eps, dres, out)
         w = "rmsnorm_backward"
+        r = self._fast.rmsnorm_backward(self._index, self._at, self._bytes, dy, h, gain, eps, dres, out)
+        if r is not None:
+            return r if r.__class__ is not int else _check(r, w)
         ph, ldh = self._matrix(w, "h", h, _TYPES)
         shape, same = h.shape, (h.dtype,)
         T, D = shape
@@ -221,6 +236,9 @@ class Ops:
             with self._on(stream):
                 return self.dequantize_rows(q, scales, dtype, out)
         w = "dequantize_rows"
+        r = self._fast.dequantize_rows(self._index, q, scales, _TYPES.get(dtype, -1), out)
+        if r is not None:
+            return r if r.__class__ is not int else _check(r, w)
         pq, ldq = self._matrix(w, "q", q, (torch.int8,))
         T, D = q.shape
         ps = self._vector(w, "scales", scales, T, (torch.float32,))
@@ -237,6 +255,10 @@ class Ops:
             with self._on(stream):
                 return self.matmul_quant(xq, xs, wq, ws, dtype, out)
         w = "matmul_quant"
+        r = self._fast.matmul_quant(self._index, self._at, self._bytes, self._status_word(), xq, xs, wq, ws,
+                                    _TYPES.get(dtype, -1), out)
+        if r is not None:
+            return r if r.__class__ is not int else _check(r, w)
         px, ldx = self._matrix(w, "xq", xq, (torch.int8,))
         T, K = xq.shape
         pw, ldw = self._matrix(w, "wq", wq, (torch.int8,))
@@ -267,13 +289,17 @@ class Ops:
             with self._on(stream):
                 return self.softmax_loss(logits, targets, weights, ignore_index, reduction, grad, grad_dtype, out)
         w = "softmax_loss"
+        if reduction not in ("mean", "sum"):
+            raise _Refused(w, f"reduction {reduction!r} is neither 'mean' nor 'sum'")
+        dt = grad_dtype or (logits.dtype if out is None else out.dtype)
+        r = self._fast.softmax_loss(self._index, self._at, self._bytes, self._status_word(), logits, targets, weights,
+                                    ignore_index, reduction == "mean", _TYPES.get(dt, -2) if grad else -1, out)
+        if r is not None:
+            return r if r.__class__ is not int else _check(r, w)
         pz, ldz = self._matrix(w, "logits", logits, _TYPES)
         T, V = logits.shape
         py = self._vector(w, "targets", targets, T, _IDS)
         pw = None if weights is None else self._vector(w, "weights", weights, T, (torch.float32,))
-        if reduction not in ("mean", "sum"):
-            raise _Refused(w, f"reduction {reduction!r} is neither 'mean' nor 'sum'")
-        dt = grad_dtype or (logits.dtype if out is None else out.dtype)
         if dt not in _TYPES:
             raise _Refused(w, f"a gradient of type {dt}", EMBER_ERR_DTYPE)
         d, pd, ldd = None, None, 0
@@ -328,6 +354,9 @@ class Ops:
                 return self.grad_norm(tensors)
         w = "grad_norm"
         tensors = list(tensors)
+        r = self._fast.grad_norm(self._index, self._at, self._bytes, tensors)
+        if r is not None:
+            return r if r.__class__ is not int else _check(r, w)
         ptrs, _, numel, types = self._list(w, tensors, None)
         norm = self._new((), torch.float32)
         n = len(tensors)
@@ -345,6 +374,9 @@ class Ops:
                 return self.clip_grads(tensors, max_norm, out, eps)
         w = "clip_grads"
         tensors = list(tensors)
+        r = self._fast.clip_grads(self._index, self._at, self._bytes, tensors, max_norm, eps, out)
+        if r is not None:
+            return r if r.__class__ is not int else _check(r, w)
         ptrs, outs, numel, types = self._list(w, tensors, out)
         norm = self._new((), torch.float32)
         n = len(tensors)

@@ -756,3 +756,119 @@ def test_a_wait_that_gives_up_is_reported(cuda_device, T, V, K):
         for a, b in zip(ops.softmax_loss(z, y), wanted):
             assert torch.equal(a, b)
         assert ops.device_status() == E.EMBER_OK
+
+
+class _Passes:
+    """A binding that takes no call."""
+
+    def __getattr__(self, name):
+        return lambda *a: None
+
+
+class _Counts:
+    """The binding, with the names of the calls it took."""
+
+    def __init__(self, binding):
+        self.binding, self.took = binding, []
+
+    def __getattr__(self, name):
+        f = getattr(self.binding, name)
+
+        def call(*a):
+            r = f(*a)
+            if r is not None:
+                self.took.append(name)
+            return r
+        return call
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [96, 1003])
+def test_compiled_calls_give_what_the_others_give(dtype, D):
+    """Every operator through the compiled call and through the module's own
+    marshalling: equal bits, shapes, strides and types."""
+    from paper_2607_01455_gb300 import Ops
+    g = torch.Generator(device="cuda")
+    g.manual_seed(D)
+
+    def new(*shape):
+        return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+    T, V = 37, 517
+    x, res, dy, gain = new(T, D), new(T, D), new(T, D), new(D)
+    z, w = new(T, V), torch.rand(T, generator=g, device="cuda")
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    padded = torch.zeros(T, V + 11, device="cuda", dtype=dtype)[:, :V].copy_(z)
+    grads = [new(n) for n in (1, 7, 4096, 0, 33)]
+    W = new(V, D)
+
+    def run(o):
+        wq, ws = o.quantize_rows(W)
+        xq, xs, _ = o.rmsnorm_quant(x, gain)
+        outs = [torch.empty_like(t) for t in grads]
+        results = [
+            *o.rmsnorm(x, gain, residual=res), *o.rmsnorm(x, None), *o.rmsnorm_quant(x, gain, residual=res),
+            *o.rmsnorm_backward(dy, x, gain), *o.rmsnorm_backward(dy, x, None, dres=res, out=torch.empty_like(x)),
+            o.dequantize_rows(xq, xs, dtype), o.matmul_quant(xq, xs, wq, ws, dtype),
+            *o.softmax_loss(z, y), *o.softmax_loss(padded, y, weights=w, reduction="sum", grad_dtype=torch.float32),
+            *o.softmax_loss(z, y.int(), grad=False), o.grad_norm(grads), o.clip_grads(grads, 0.5, out=outs), *outs]
+        assert o.device_status() == 0
+        return results
+
+    a, b = Ops(), Ops()
+    a._fast, b._fast = _Counts(a._fast), _Passes()
+    run(a)  # the workspace grows on the way
+    a._fast.took.clear()
+    for p, q in zip(run(a), run(b), strict=True):
+        assert (p is None) == (q is None)
+        if p is not None:
+            assert p.shape == q.shape and p.stride() == q.stride() and p.dtype == q.dtype and torch.equal(p, q)
+    assert a._fast.took == ["rmsnorm_quant", "rmsnorm", "rmsnorm", "rmsnorm_quant", "rmsnorm_backward",
+                            "rmsnorm_backward", "dequantize_rows", "matmul_quant", "softmax_loss", "softmax_loss",
+                            "softmax_loss", "grad_norm", "clip_grads"]
+
+
+@pytest.mark.gpu
+def test_compiled_calls_keep_no_references():
+    import sys
+
+    from paper_2607_01455_gb300 import Ops
+    o = Ops()
+    x, out, gain = torch.randn(5, 64, device="cuda"), torch.empty(5, 64, device="cuda"), torch.ones(64, device="cuda")
+    grads = [torch.randn(9, device="cuda") for _ in range(3)]
+    y = torch.zeros(5, dtype=torch.int64, device="cuda")
+    held = [x, out, gain, grads, grads[0], y]
+
+    def calls():
+        o.rmsnorm(x, gain, out=out)
+        o.rmsnorm(x, gain, residual=x, residual_out=out)
+        o.rmsnorm_quant(x, gain)
+        o.rmsnorm_backward(x, x, gain, out=out)
+        o.softmax_loss(x, y, out=out)
+        o.clip_grads(grads, 1.0)
+        with pytest.raises(Exception):
+            o.rmsnorm(x, gain, out=out[:4])
+
+    calls()
+    before = [sys.getrefcount(t) for t in held]
+    torch.cuda.synchronize()
+    memory = torch.cuda.memory_allocated()
+    for _ in range(8):
+        calls()
+    torch.cuda.synchronize()
+    assert [sys.getrefcount(t) for t in held] == before and torch.cuda.memory_allocated() == memory
+
+
+@pytest.mark.gpu
+def test_clipping_refuses_a_limit_that_is_no_number():
+    import ctypes
+
+    from paper_2607_01455_gb300 import Ops
+    o = Ops()
+    grads = [torch.ones(4, device="cuda")]
+    o.clip_grads(grads, 8.0)
+    for bad in (None, "1"):
+        with pytest.raises((TypeError, ctypes.ArgumentError)):
+            o.clip_grads(grads, bad)
+    assert torch.equal(grads[0], torch.ones(4, device="cuda"))

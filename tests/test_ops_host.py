@@ -142,3 +142,28 @@ def test_the_python_layer_names_what_it_refuses():
     with pytest.raises(E.EmberError) as ex:
         o._list("f", [z.double()], None)
     assert ex.value.status == DTYPE
+
+
+def test_binding_passes_on_what_is_not_on_its_device():
+    """Arguments that are no CUDA tensors are left to the module, which names what is wrong."""
+    import torch
+
+    from paper_2607_01455_gb300 import ember
+    b = ember.ops_binding()
+    x, n = torch.zeros(2, 8), torch.zeros(8)
+    q, s, y = torch.zeros(2, 8, dtype=torch.int8), torch.zeros(2), torch.zeros(2, dtype=torch.int64)
+    big = 1 << 30
+    assert b.rmsnorm(0, x, n, None, 1e-6, None, None) is None
+    assert b.rmsnorm(0, None, n, None, 1e-6, None, None) is None
+    assert b.rmsnorm_quant(0, x, n, None, 1e-6, None) is None
+    assert b.rmsnorm_backward(0, 0, big, x, x, n, 1e-6, None, None) is None
+    assert b.dequantize_rows(0, q, s, 0, None) is None
+    assert b.matmul_quant(0, 0, big, 0, q, s, q, s, 0, None) is None
+    assert b.softmax_loss(0, 0, big, 0, x, y, None, -100, True, 0, None) is None
+    assert b.grad_norm(0, 0, big, [x]) is None
+    assert b.clip_grads(0, 0, big, [x], 1.0, 1e-6, None) is None
+    assert b.clip_grads(0, 0, big, [x], 1.0, 1e-6, [x, x]) is None
+    with pytest.raises(TypeError):
+        b.rmsnorm(0, x)
+    with pytest.raises(TypeError):
+        b.bind(1)
