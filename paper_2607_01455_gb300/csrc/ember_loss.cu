@@ -127,9 +127,12 @@ __device__ __forceinline__ int counted(const LossArgs &a)
 __device__ __forceinline__ double loss_sum(const LossArgs &a, int64_t first, int64_t step, double *part)
 {
     double s = 0.0;
-    for (int64_t t = first; t < a.T; t += step)
-        if (counts(a, target_of(a, t)))
-            s += (double)__ldcg(a.nll + t) * (a.w ? (double)a.w[t] : 1.0);
+#pragma unroll 4
+    for (int64_t t = first; t < a.T; t += step) {  // the loads of four tokens at once
+        const int64_t y = target_of(a, t);
+        const float nll = __ldcg(a.nll + t), w = a.w ? a.w[t] : 1.f;
+        s += counts(a, y) ? (double)nll * (double)w : 0.0;
+    }
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1)
         s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -368,8 +371,10 @@ k_loss_rows(LossArgs a)
     }
     if (C > 1)
         tc::cluster_arrive_release();  // waited for before the first store into another CTA: by then all are ready
-    dev::grid_dep_wait();
-    dev::grid_dep_launch();
+    if constexpr (HERE) {  // otherwise the kernel before is k_loss_count, and only its result is waited for
+        dev::grid_dep_wait();
+        dev::grid_dep_launch();
+    }
 
     // The copy of row t's slice, by thread 0; rows that do not count need none.
     uint32_t started = 0;
@@ -402,6 +407,7 @@ k_loss_rows(LossArgs a)
         __shared__ int nvalid[32];
         int c = 0;
         bool bad = false;
+#pragma unroll 4
         for (int64_t q = tid; q < a.T; q += nt) {
             const int64_t yq = target_of(a, q);
             c += counts(a, yq);
@@ -420,6 +426,8 @@ k_loss_rows(LossArgs a)
         if (blockIdx.x == 0 && tid == 0)
             *a.count = c;
     } else {
+        dev::grid_dep_wait();
+        dev::grid_dep_launch();
         if (a.mean)
             n = (float)counted(a);
         __syncthreads();  // the mbarriers are initialised
@@ -601,9 +609,13 @@ struct RowPlan {
 };
 // Up to so many tokens are one launch: every CTA counts the targets itself and
 // the last one adds up the losses (127 x 50257 fp32: 18.2 us, with launches of
-// their own for both 21.6).  More would keep a CTA busy for longer than the
-// launches take.
-constexpr int64_t kFewRowsHere = 512;
+// their own for both 21.6; 1000 x 8000 bf16 16.5 and 16.9, 2000 x 8000 fp32 34
+// and 32).  More would keep a CTA busy for longer than the launches take.
+constexpr int64_t kFewRowsHere = 1024;
+// So would more than these per thread of a CTA, short rows having small ones
+// (one warp, 1000 fp32: 400 rows 9.9 us, with the launches 11.3; 500 rows 12.5
+// and 11.7).
+constexpr int64_t kFewPerThread = 12;
 
 RowPlan row_plan(int64_t T, int64_t V, int esize)
 {
@@ -672,7 +684,7 @@ cudaError_t launch_rows(LossArgs a, cudaStream_t stream)
     constexpr int VE = 16 / sizeof(ZT);
     if (GRAD && (((uintptr_t)a.z / sizeof(ZT) - (uintptr_t)a.d / sizeof(DT)) % VE != 0 || (a.ldz - a.ldd) % VE != 0))
         p.C = 0;
-    const bool here = p.C > 0 && a.T <= kFewRowsHere;
+    const bool here = p.C > 0 && a.T <= kFewRowsHere && a.T <= kFewPerThread * p.nt;
     a.nparts = here ? 1 : (int)(a.T / kPartTokens < kMaxParts ? a.T / kPartTokens + 1 : kMaxParts);
     cudaError_t e = cudaSuccess;
     if (!here)

@@ -872,3 +872,30 @@ def test_clipping_refuses_a_limit_that_is_no_number():
         with pytest.raises((TypeError, ctypes.ArgumentError)):
             o.clip_grads(grads, bad)
     assert torch.equal(grads[0], torch.ones(4, device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,V", [(384, 300), (385, 300), (513, 5003), (1024, 8000), (1025, 8000), (1100, 1000), (5000, 129)])
+@pytest.mark.parametrize("zt", [BF, F32])
+def test_loss_with_and_without_launches_of_its_own_for_the_count(ops, T, V, zt):
+    """Numbers of tokens around the limits up to which one launch does it all;
+    weights of tokens that do not count reach nothing, not as NaN either."""
+    g = gen(T + V)
+    z = rows(g, T, V, zt, scale=3.0)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    w = randn(g, T)
+    ignored = torch.arange(T, device="cuda") % 7 == 3
+    y[ignored] = -100
+    check_loss(ops, z, y)
+    w64 = torch.where(ignored, 0.0, w)
+    w[ignored] = float("nan")
+    got = ops.softmax_loss(z, y, weights=w)
+    want = check_loss(ops, z, y, w64)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert ops.device_status() == E.EMBER_OK
+    y[5] = V
+    loss, nll, d = ops.softmax_loss(z, y)
+    y[5] = -100
+    assert torch.equal(loss, ops.softmax_loss(z, y)[0]) and nll[5] == 0 and (d[5] == 0).all()
+    assert ops.device_status() == E.EMBER_ERR_ID_OUT_OF_RANGE
