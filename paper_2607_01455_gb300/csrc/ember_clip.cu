@@ -28,8 +28,9 @@ using namespace rows;
 
 constexpr int kClipThreads = 512;
 constexpr int kClipCtas = kSms * 2;
-constexpr int kFewTensors = 64;
-constexpr int kManyTensors = 1024;
+// Tensors of a launch: the host copies the whole list for each (clipping 100
+// tensors of 1000 with 256 places 8.8 us, with 1024 10.7).
+constexpr int kFewTensors = 64, kSomeTensors = 256, kManyTensors = 1024;
 
 template <int CAP>
 struct TensorList {
@@ -384,12 +385,15 @@ cudaError_t run(const Tensors &t, bool scale, const ClipArgs &a, cudaStream_t st
     int64_t total = 0;
     for (int k = 0; k < t.n; ++k)
         total += t.numel[k];
-    const bool few = t.n <= kFewTensors;
-    if (total < 4 * kClipCtas * kSmallChunk)
-        return few ? passes<kFewTensors, 1>(t, kSmallChunk, scale, a, stream)
-                   : passes<kManyTensors, 1>(t, kSmallChunk, scale, a, stream);
-    return few ? passes<kFewTensors, 4>(t, kLargeChunk, scale, a, stream)
-               : passes<kManyTensors, 4>(t, kLargeChunk, scale, a, stream);
+    const bool brief = total < 4 * kClipCtas * kSmallChunk;
+    if (t.n <= kFewTensors)
+        return brief ? passes<kFewTensors, 1>(t, kSmallChunk, scale, a, stream)
+                     : passes<kFewTensors, 4>(t, kLargeChunk, scale, a, stream);
+    if (t.n <= kSomeTensors)
+        return brief ? passes<kSomeTensors, 1>(t, kSmallChunk, scale, a, stream)
+                     : passes<kSomeTensors, 4>(t, kLargeChunk, scale, a, stream);
+    return brief ? passes<kManyTensors, 1>(t, kSmallChunk, scale, a, stream)
+                 : passes<kManyTensors, 4>(t, kLargeChunk, scale, a, stream);
 }
 
 }  // namespace

@@ -899,3 +899,13 @@ def test_loss_with_and_without_launches_of_its_own_for_the_count(ops, T, V, zt):
     y[5] = -100
     assert torch.equal(loss, ops.softmax_loss(z, y)[0]) and nll[5] == 0 and (d[5] == 0).all()
     assert ops.device_status() == E.EMBER_ERR_ID_OUT_OF_RANGE
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [63, 64, 65, 256, 257, 1024, 1025])
+def test_clip_around_the_launches_limits(ops, n):
+    """Numbers of tensors at which the next longer list, or another launch, begins."""
+    g = gen(n)
+    grads = [randn(g, 1 + (53 * k) % 211).to(BF if k % 4 == 1 else F32) for k in range(n)]
+    check_clip(ops, grads, 0.7)
+    check_clip(ops, grads[:-1] + [randn(g, 6000000)], 0.7, in_place=True)
