@@ -100,8 +100,8 @@ __global__ void __launch_bounds__(256) k_mm_any(MmArgs a, int obf16, unsigned vb
 
 
 // ---------------------------------------------------------------------------
-// Few tokens.  The tokens' rows sit in shared memory, zero-padded to whole
-// 512-byte slabs; a warp takes R rows of the table at a time, 16 bytes of each
+// Few tokens, a row of the grid per group of TN.  The tokens' rows sit in shared
+// memory, zero-padded to whole 512-byte slabs; a warp takes R rows of the table at a time, 16 bytes of each
 // row per lane and slab, so that every 16 bytes of x are read from shared
 // memory once for R rows.  The lanes' integer sums are joined by a transposed
 // butterfly: R TN totals for about as many shuffles.  Bound by HBM for one to
@@ -156,11 +156,12 @@ __global__ void __launch_bounds__(kFewThreads, MINB) k_mm_few(MmArgs a, int obf1
 {
     extern __shared__ __align__(16) int8_t sx[];  // [TN][kpad]
     const int lane = threadIdx.x & 31;
+    const int t0 = blockIdx.y * TN, nt = (int)a.T - t0;  // this CTA's tokens
     dev::grid_dep_wait();
     dev::grid_dep_launch();
     for (int t = 0; t < TN; ++t) {
-        const int8_t *row = a.xq + t * a.ldx;
-        const bool on = t < a.T;
+        const int8_t *row = a.xq + (t0 + t) * a.ldx;
+        const bool on = t < nt;
         if (on && (uintptr_t)row % 16 == 0) {
             for (int k = threadIdx.x * 16; k < kpad; k += kFewThreads * 16) {
                 int4 v = make_int4(0, 0, 0, 0);
@@ -215,8 +216,8 @@ __global__ void __launch_bounds__(kFewThreads, MINB) k_mm_few(MmArgs a, int obf1
         const int sum = warp_isum_transposed<R * TN>(acc, lane, index);
         const int64_t v = q * R + index / TN;
         const int t = index % TN;
-        if (lane % (32 / (R * TN)) == 0 && v < a.V && t < a.T)
-            store_out(a.out, obf16, t * a.ldo + v, (float)sum * a.xs[t] * a.ws[v]);
+        if (lane % (32 / (R * TN)) == 0 && v < a.V && t < nt)
+            store_out(a.out, obf16, (t0 + t) * a.ldo + v, (float)sum * a.xs[t0 + t] * a.ws[v]);
     }
 }
 
@@ -853,6 +854,9 @@ cudaError_t launch_tc(const MmArgs &m, int obf16, void *workspace, unsigned *fla
     return e;
 }
 
+// CTAs of k_mm_few with R rows of the table per warp.
+int64_t few_ctas(int64_t V, int R) { return ((V + R - 1) / R + kFewThreads / 32 - 1) / (kFewThreads / 32); }
+
 template <int TN, int R, int MINB, int UNR>
 cudaError_t launch_few(const MmArgs &a, int obf16, int kpad, cudaStream_t stream)
 {
@@ -860,9 +864,9 @@ cudaError_t launch_few(const MmArgs &a, int obf16, int kpad, cudaStream_t stream
         cudaFuncSetAttribute(k_mm_few<TN, R, MINB, UNR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
     if (e != cudaSuccess)
         return e;
-    const int64_t ctas = ((a.V + R - 1) / R + kFewThreads / 32 - 1) / (kFewThreads / 32);
-    return launch_k(k_mm_few<TN, R, MINB, UNR>, dim3((unsigned)(ctas < MINB * kSms ? ctas : MINB * kSms)), dim3(kFewThreads),
-                    (size_t)TN * kpad, stream, true, a, obf16, kpad);
+    const int64_t ctas = few_ctas(a.V, R);
+    const dim3 grid((unsigned)(ctas < MINB * kSms ? ctas : MINB * kSms), (unsigned)((a.T + TN - 1) / TN));
+    return launch_k(k_mm_few<TN, R, MINB, UNR>, grid, dim3(kFewThreads), (size_t)TN * kpad, stream, true, a, obf16, kpad);
 }
 
 // Rows per warp, CTAs per SM and unrolled slabs of k_mm_few, measured on
@@ -873,11 +877,17 @@ cudaError_t launch_few(const MmArgs &a, int obf16, int kpad, cudaStream_t stream
 //   4 rows, 4 CTAs, 4 slabs   24 /  - /  -    162 /   - /   -
 //   8 rows, 2 CTAs, 4 slabs   25 / 29 /  -    158 / 166 /   -
 //   k_mm_tc                   31 / 31 / 31    179 / 179 / 180
-// Five to eight tokens go to the tensor cores for large tables (k_mm_few / k_mm_tc
-// for 6 tokens: 10000 x 2048 9.0 / 12.6, 40000 x 8192 75 / 81, 50257 x 768 16.6 /
-// 13.7).
+// Five to eight tokens go to the tensor cores for large tables, of short rows
+// sooner (k_mm_few / k_mm_tc for 6 tokens: 10000 x 2048 9.0 / 12.6, 40000 x 8192
+// 75 / 81, 50257 x 768 16.6 / 13.7, 8000 x 512 4.9 / 6.7, 32000 x 256 9.2 / 7.0).
+// More tokens stay here in groups of eight while all groups run at once and
+// the rows are short: the tensor cores' two launches take longer to begin
+// (16 tokens: 1000 x 2048 5.6 / 10.9, 4000 x 512 5.1 / 6.6, 4000 x 2048 7.2 /
+// 11.1, 1000 x 8192 12.3 / 10.4; 64 and 100 tokens: 1000 x 512 5.1 / 6.9 and, in
+// more than one wave, 8.9 / 8.0).
 constexpr int kFewShortRow = 2048;
-constexpr int64_t kFewMaxRows = 49152;
+constexpr int64_t kFewMaxRows = 49152, kFewMaxShortRows = 16384;
+constexpr int kFewR = 4, kFewMinB = 2;  // of the form for eight tokens
 
 cudaError_t launch_mm(const MmArgs &a, int obf16, void *workspace, unsigned *flags, cudaStream_t stream)
 {
@@ -890,8 +900,11 @@ cudaError_t launch_mm(const MmArgs &a, int obf16, void *workspace, unsigned *fla
             return brief ? launch_few<2, 8, 2, 4>(a, obf16, kpad, stream) : launch_few<2, 4, 2, 2>(a, obf16, kpad, stream);
         if (a.T <= 4 && (size_t)4 * kpad <= kFewSmem)
             return brief ? launch_few<4, 8, 2, 4>(a, obf16, kpad, stream) : launch_few<4, 4, 2, 2>(a, obf16, kpad, stream);
-        if (a.T <= kFewTokens && a.V <= kFewMaxRows && (size_t)kFewTokens * kpad <= kFewSmem)
-            return launch_few<kFewTokens, 4, 2, 4>(a, obf16, kpad, stream);
+        const int64_t groups = (a.T + kFewTokens - 1) / kFewTokens;
+        const bool few = groups == 1 ? a.V <= (a.K < 1024 ? kFewMaxShortRows : kFewMaxRows)
+                                     : brief && few_ctas(a.V, kFewR) * groups <= kFewMinB * kSms;
+        if (few && (size_t)kFewTokens * kpad <= kFewSmem)
+            return launch_few<kFewTokens, kFewR, kFewMinB, 4>(a, obf16, kpad, stream);
         return launch_tc(a, obf16, workspace, flags, stream);
     }
     const int64_t vb = (a.V + kGV - 1) / kGV, tb = (a.T + kGT - 1) / kGT;

@@ -909,3 +909,21 @@ def test_clip_around_the_launches_limits(ops, n):
     grads = [randn(g, 1 + (53 * k) % 211).to(BF if k % 4 == 1 else F32) for k in range(n)]
     check_clip(ops, grads, 0.7)
     check_clip(ops, grads[:-1] + [randn(g, 6000000)], 0.7, in_place=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,V,K", [(9, 1000, 64), (16, 4863, 2048), (24, 1000, 512), (76, 1000, 272), (72, 1024, 1003),
+                                   (73, 1056, 2048), (7, 16385, 1008), (8, 16384, 100), (300, 33, 640), (304, 8, 16)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_product_of_token_groups(ops, T, V, K, dtype):
+    """More than eight tokens by a small table, around the limits of the form that takes them in groups."""
+    g = gen(T + V + K)
+    ld = (K + 15) // 16 * 16
+    x, w = ints(g, T, K, ld), ints(g, V, K, ld)
+    check_product(ops, x, w, g, dtype)
+    xs, ws = torch.rand(T, generator=g, device="cuda"), torch.rand(V, generator=g, device="cuda")
+    guard = torch.full((T + 3, V + 5), 7.0, device="cuda", dtype=dtype)
+    out = ops.matmul_quant(x, xs, w, ws, dtype=dtype, out=guard[1:T + 1, 2:V + 2])
+    assert torch.equal(out, ops.matmul_quant(x, xs, w, ws, dtype=dtype))
+    guard[1:T + 1, 2:V + 2] = 7
+    assert (guard == 7).all()
