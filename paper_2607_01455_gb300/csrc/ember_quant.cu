@@ -101,11 +101,11 @@ __global__ void __launch_bounds__(256) k_mm_any(MmArgs a, int obf16, unsigned vb
 
 // ---------------------------------------------------------------------------
 // Few tokens, a row of the grid per group of TN.  The tokens' rows sit in shared
-// memory, zero-padded to whole 512-byte slabs; a warp takes R rows of the table at a time, 16 bytes of each
-// row per lane and slab, so that every 16 bytes of x are read from shared
-// memory once for R rows.  The lanes' integer sums are joined by a transposed
-// butterfly: R TN totals for about as many shuffles.  Bound by HBM for one to
-// four tokens: 128256 x 8192 for one token 149 us, 7.1 TB/s; for eight, dp4a
+// memory, zero-padded to whole 512-byte slabs; a warp takes R rows of the table
+// at a time, 16 bytes of each row per lane and slab, so that every 16 bytes of x
+// are read from shared memory once for R rows.  The lanes' integer sums are
+// joined by a transposed butterfly: R TN totals for about as many shuffles.
+// Bound by HBM for one to four tokens: 128256 x 8192 for one token 149 us, 7.1 TB/s; for eight, dp4a
 // sets the pace (195 us).
 // ---------------------------------------------------------------------------
 constexpr int kFewTokens = 8;

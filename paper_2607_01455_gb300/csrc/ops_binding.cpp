@@ -18,6 +18,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
 #include <c10/cuda/CUDAStream.h>
+#include <c10/util/Exception.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -168,8 +169,10 @@ PyObject *tuple3(Refs &r)
         if (!(condition))   \
             Py_RETURN_NONE; \
     } while (0)
+// Without the interpreter's lock: the call takes C values alone.
 #define LAUNCHED(call)                         \
     do {                                       \
+        void *const stream = stream_of(index); \
         ember_status st_;                      \
         Py_BEGIN_ALLOW_THREADS st_ = (call);   \
         Py_END_ALLOW_THREADS                   \
@@ -199,9 +202,10 @@ PyObject *rmsnorm(PyObject *const *a)
     Refs refs;
     COMMON(PyFloat_Check(a[4]) && matrix(a[1], index, x) && is_float(x.type) && gain_of(a[2], index, x.cols, gain, gtype) &&
            residual_of(a[3], a[6], index, x, q, refs.r[1]) && output(a[5], index, x, x.type, y, refs.r[0]));
+    const float eps = (float)PyFloat_AS_DOUBLE(a[4]);
     LAUNCHED(lib.rmsnorm(x.p, x.ld, (ember_wdtype)x.type, q.r.p, q.r.ld, (ember_wdtype)q.r.type, gain,
-                         (ember_wdtype)gtype, x.rows, x.cols, (float)PyFloat_AS_DOUBLE(a[4]), q.h.p, q.h.ld, y.p, y.ld,
-                         stream_of(index)));
+                         (ember_wdtype)gtype, x.rows, x.cols, eps, q.h.p, q.h.ld, y.p, y.ld,
+                         stream));
     return tuple2(refs);
 }
 
@@ -218,10 +222,11 @@ PyObject *rmsnorm_quant(PyObject *const *a)
            residual_of(a[3], a[5], index, x, q, refs.r[2]));
     const int64_t ld = (x.cols + 15) / 16 * 16;
     Tensor v = at::empty({x.rows, ld}, on(index, at::kChar)), s = at::empty({x.rows}, on(index, at::kFloat));
+    const float eps = (float)PyFloat_AS_DOUBLE(a[4]);
     LAUNCHED(lib.rmsnorm_quant(x.p, x.ld, (ember_wdtype)x.type, q.r.p, q.r.ld, (ember_wdtype)q.r.type, gain,
-                               (ember_wdtype)gtype, x.rows, x.cols, (float)PyFloat_AS_DOUBLE(a[4]), q.h.p, q.h.ld,
+                               (ember_wdtype)gtype, x.rows, x.cols, eps, q.h.p, q.h.ld,
                                static_cast<int8_t *>(v.data_ptr()), ld, static_cast<float *>(s.data_ptr()),
-                               stream_of(index)));
+                               stream));
     refs.r[0] = THPVariable_Wrap(ld == x.cols ? v : v.narrow(1, 0, x.cols));
     refs.r[1] = THPVariable_Wrap(std::move(s));
     return tuple3(refs);
@@ -241,9 +246,11 @@ PyObject *rmsnorm_backward(PyObject *const *a)
            (a[7] == Py_None || (matrix(a[7], index, dres) && like(dres, h, h.type))));
     COMMON(lib.back_bytes(h.rows, h.cols) <= bytes && output(a[8], index, h, h.type, dx, refs.r[0]));
     Tensor g = at::empty({h.cols}, on(index, at::kFloat));
+    const float eps = (float)PyFloat_AS_DOUBLE(a[6]);
+    void *work = (void *)PyLong_AsLongLong(a[1]);
     LAUNCHED(lib.back(dy.p, dy.ld, h.p, h.ld, dres.p, dres.ld, (ember_wdtype)h.type, gain, (ember_wdtype)gtype, h.rows,
-                      h.cols, (float)PyFloat_AS_DOUBLE(a[6]), dx.p, dx.ld, static_cast<float *>(g.data_ptr()),
-                      (void *)PyLong_AsLongLong(a[1]), bytes, stream_of(index)));
+                      h.cols, eps, dx.p, dx.ld, static_cast<float *>(g.data_ptr()),
+                      work, bytes, stream));
     refs.r[1] = THPVariable_Wrap(std::move(g));
     return tuple2(refs);
 }
@@ -259,7 +266,7 @@ PyObject *dequantize_rows(PyObject *const *a)
     COMMON(is_float(type) && matrix(a[1], index, q) && q.type == kInt8 && floats(a[2], index, q.rows, s) &&
            output(a[4], index, q, type, y, refs.r[0]));
     LAUNCHED(lib.dequantize(static_cast<int8_t *>(q.p), q.ld, static_cast<float *>(s), q.rows, q.cols, y.p, y.ld,
-                            (ember_wdtype)type, stream_of(index)));
+                            (ember_wdtype)type, stream));
     return refs.take(0);
 }
 
@@ -278,9 +285,11 @@ PyObject *matmul_quant(PyObject *const *a)
     shape.rows = x.rows;
     shape.cols = w.rows;
     COMMON(lib.matmul_bytes(x.rows, w.rows, x.cols) <= bytes && output(a[9], index, shape, type, o, refs.r[0]));
+    void *work = (void *)PyLong_AsLongLong(a[1]);
+    unsigned *status = (unsigned *)PyLong_AsLongLong(a[3]);
     LAUNCHED(lib.matmul(static_cast<int8_t *>(x.p), x.ld, static_cast<float *>(xs), static_cast<int8_t *>(w.p), w.ld,
                         static_cast<float *>(ws), x.rows, w.rows, x.cols, o.p, o.ld, (ember_wdtype)type,
-                        (void *)PyLong_AsLongLong(a[1]), bytes, (unsigned *)PyLong_AsLongLong(a[3]), stream_of(index)));
+                        work, bytes, status, stream));
     return refs.take(0);
 }
 
@@ -313,11 +322,13 @@ PyObject *softmax_loss(PyObject *const *a)
             COMMON(output(a[10], index, z, type, d, refs.r[2]));
     }
     Tensor loss = at::empty({}, on(index, at::kFloat)), nll = at::empty({z.rows}, on(index, at::kFloat));
+    const int mean = PyObject_IsTrue(a[8]);
+    void *work = (void *)PyLong_AsLongLong(a[1]);
+    unsigned *status = (unsigned *)PyLong_AsLongLong(a[3]);
     LAUNCHED(lib.loss(z.p, z.ld, (ember_wdtype)z.type, y, yt == at::kLong ? EMBER_I64 : EMBER_I32,
-                      static_cast<float *>(w), ignore, PyObject_IsTrue(a[8]), z.rows, z.cols,
+                      static_cast<float *>(w), ignore, mean, z.rows, z.cols,
                       static_cast<float *>(loss.data_ptr()), static_cast<float *>(nll.data_ptr()), d.p, d.ld,
-                      (ember_wdtype)(type >= 0 ? type : EMBER_F32), (void *)PyLong_AsLongLong(a[1]), bytes,
-                      (unsigned *)PyLong_AsLongLong(a[3]), stream_of(index)));
+                      (ember_wdtype)(type >= 0 ? type : EMBER_F32), work, bytes, status, stream));
     refs.r[0] = THPVariable_Wrap(std::move(loss));
     refs.r[1] = THPVariable_Wrap(std::move(nll));
     return tuple3(refs);
@@ -361,11 +372,12 @@ PyObject *clip(PyObject *const *a)
     Tensor norm = at::empty({}, on(index, at::kFloat));
     float *np = static_cast<float *>(norm.data_ptr());
     void *ws = (void *)PyLong_AsLongLong(a[1]);
-    if constexpr (SCALE)
-        LAUNCHED(lib.clip((int)n, in.data(), out.data(), numel.data(), types.data(), (float)PyFloat_AS_DOUBLE(a[4]),
-                          (float)PyFloat_AS_DOUBLE(a[5]), np, ws, bytes, stream_of(index)));
-    else
-        LAUNCHED(lib.norm((int)n, in.data(), numel.data(), types.data(), np, ws, bytes, stream_of(index)));
+    if constexpr (SCALE) {
+        const float max_norm = (float)PyFloat_AS_DOUBLE(a[4]), eps = (float)PyFloat_AS_DOUBLE(a[5]);
+        LAUNCHED(lib.clip((int)n, in.data(), out.data(), numel.data(), types.data(), max_norm, eps, np, ws, bytes,
+                          stream));
+    } else
+        LAUNCHED(lib.norm((int)n, in.data(), numel.data(), types.data(), np, ws, bytes, stream));
     return THPVariable_Wrap(std::move(norm));
 }
 
@@ -378,11 +390,16 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
     }
     try {
         return F(args);
+    } catch (const c10::OutOfMemoryError &) {
+        Py_RETURN_NONE;  // before the launch; the module's own path raises torch's exception
     } catch (const std::exception &e) {
         if (!PyErr_Occurred())
             PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
+    } catch (...) {
+        if (!PyErr_Occurred())
+            PyErr_SetString(PyExc_RuntimeError, "unknown exception");
     }
+    return nullptr;
 }
 
 // (addresses of the functions of `lib`, in order)
