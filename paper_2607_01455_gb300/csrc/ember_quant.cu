@@ -105,8 +105,8 @@ __global__ void __launch_bounds__(256) k_mm_any(MmArgs a, int obf16, unsigned vb
 // at a time, 16 bytes of each row per lane and slab, so that every 16 bytes of x
 // are read from shared memory once for R rows.  The lanes' integer sums are
 // joined by a transposed butterfly: R TN totals for about as many shuffles.
-// Bound by HBM for one to four tokens: 128256 x 8192 for one token 149 us, 7.1 TB/s; for eight, dp4a
-// sets the pace (195 us).
+// Bound by HBM for one to four tokens: 128256 x 8192 for one token 145 us, 7.2
+// TB/s; for eight, dp4a sets the pace (195 us).
 // ---------------------------------------------------------------------------
 constexpr int kFewTokens = 8;
 constexpr int kFewThreads = 256;
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kFewThreads, MINB) k_mm_few(MmArgs a, int obf1
 //     columns: shared memory sees 8 bits per value of the table, not 8 + 16 + 16;
 //   - gets its half of the tokens' block, already fp16 (k_widen writes them
 //     once per call), by TMA.
-// Measured: 2048 x 32000 x 4096 321 us, 1670 TFLOP/s, 0.87 of the cuBLAS bf16
+// Measured: 2048 x 32000 x 4096 325 us, 1650 TFLOP/s, 0.86 of the cuBLAS bf16
 // burst (the tensor pipes wait for the widened blocks in between); 64 x 128256 x
 // 4096 95 us, 5.7 TB/s; 49 x 151936 x 896 33 us, 5.0 TB/s.
 // Roles (512 threads per CTA, one CTA per SM, persistent over tiles):
