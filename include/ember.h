@@ -394,9 +394,9 @@ ember_status ember_rmsnorm(const void *x, int64_t ldx, ember_wdtype xtype,
                            const void *gain, ember_wdtype gtype, int64_t T, int64_t D, float eps,
                            void *h, int64_t ldh, void *y, int64_t ldy, void *stream);
 
-/* The same with y in 8 bits: scales[t] = max_j |y_tj| / 127 and
- * q_tj = y_tj / scales[t] rounded to nearest even, |q| <= 127, so that
- * y_tj is about q_tj scales[t].  A row of zeros has the scale 0; a row with
+/* The same with y (in fp32) in 8 bits: scales[t] = max_j |y_tj| / 127 and
+ * q_tj = the fp32 quotient y_tj / scales[t] rounded to nearest even, |q| <= 127,
+ * so that y_tj is about q_tj scales[t].  A row of zeros has the scale 0; a row with
  * an infinity or a NaN has the scale NaN and zeros in q. */
 ember_status ember_rmsnorm_quant(const void *x, int64_t ldx, ember_wdtype xtype,
                                  const void *residual, int64_t ldr, ember_wdtype rtype,

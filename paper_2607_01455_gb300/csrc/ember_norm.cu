@@ -19,7 +19,7 @@
 //
 // Measured, of the copy bandwidth (6780 GB/s): norm 8192 x 4096 bf16 with an
 // fp32 residual 60.7 us, 0.98; 8192 x 8192 bf16 with residual 79 us, 1.00;
-// in 8 bits 76 us, 0.91; backward with dres 89 us, 0.89 (fp32 156 us, 1.02).
+// in 8 bits 79 us, 0.88; backward with dres 89 us, 0.89 (fp32 156 us, 1.02).
 // Rows off the 16-byte boundaries: 0.2 to 0.85 (k_rmsnorm_shifted).
 #include <type_traits>
 
@@ -53,7 +53,7 @@ __device__ __forceinline__ float row_reduce(float v, float *part, int tpr)
     return r;
 }
 
-// q = y / scale rounded to nearest even, |q| <= 127.  A row of zeros has the
+// q = y / scale rounded to fp32 and then to nearest even, |q| <= 127.  A row of zeros has the
 // scale 0 and zeros; a row with an infinity or a NaN has the scale NaN and
 // zeros, so that what is formed from it is NaN throughout.
 struct RowScale {
@@ -68,36 +68,54 @@ __device__ __forceinline__ RowScale row_scale(float top)
     s.inv = 0.f;
     if (!(top <= 3.402823466e38f)) {  // infinity or NaN
         s.scale = __uint_as_float(0x7FC00000u);
-    } else if (s.scale >= 1e-30f) {
+    } else if (s.scale >= 1e-25f) {
         s.inv = 1.f / s.scale;
-    } else if (s.scale > 0.f) {  // 1 / scale may overflow, and scale itself be subnormal
+    } else if (s.scale > 0.f) {  // 1 / scale may overflow, scale itself or a remainder be subnormal
         s.divide = true;
     }
     return s;
 }
-// The low byte of the result is q: adding 1.5 2^23 leaves the value rounded to
-// an integer, nearest even, in the low bits of the fp32 number.  |y inv| is at
-// most 127 (1 + 2^-22), so no bound is needed there.
-__device__ __forceinline__ unsigned quant(float y, const RowScale &s)
+// The codes of VEC values, in the low bytes: adding 1.5 2^23 leaves a value
+// rounded to an integer, nearest even, in the low bits of the fp32 number.  The
+// quotient is y inv with one correction by its remainder (Markstein's division):
+// the remainder is exact, so what is rounded once more is the quotient to within
+// 2^-23 of its last place, and a value next to a tie falls to its side.  (By y inv
+// alone, which is off by up to 2^-17, one code in 10^5 differs.)  |quotient| is at most 127 (1 + 2^-23), so no bound is
+// needed there.
+template <int VEC>
+__device__ __forceinline__ void quants(const float (&y)[VEC], const RowScale &s, unsigned (&q)[VEC])
 {
-    if (s.divide)
-        y = fminf(fmaxf(y / s.scale, -127.f), 127.f);
-    return __float_as_uint(fmaf(y, s.divide ? 1.f : s.inv, 12582912.f));
+    if (s.divide) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            q[e] = __float_as_uint(fminf(fmaxf(y[e] / s.scale, -127.f), 127.f) + 12582912.f);
+        return;
+    }
+    if (s.inv == 0.f) {  // zeros, also where y is infinite or NaN
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            q[e] = 0;
+        return;
+    }
+    // pairs: without a test per value 8192 x 8192 bf16 take 48 us, with one 61
+    const f2 inv = make2(s.inv, s.inv), minus = make2(-s.scale, -s.scale), magic = make2(12582912.f, 12582912.f);
+#pragma unroll
+    for (int e = 0; e < VEC; e += 2) {
+        const f2 v = make2(y[e], VEC > 1 ? y[e + (VEC > 1)] : 0.f);
+        const f2 guess = mul2(v, inv);
+        float lo, hi;
+        split2(add2(fma2(fma2(guess, minus, v), inv, guess), magic), lo, hi);
+        q[e] = __float_as_uint(lo);
+        if constexpr (VEC > 1)
+            q[e + 1] = __float_as_uint(hi);
+    }
 }
 
 template <int VEC>
 __device__ __forceinline__ void store_q(int8_t *p, const float (&y)[VEC], const RowScale &s)
 {
     unsigned q[VEC];
-    if (!s.divide && s.inv == 0.f) {  // zeros, also where y is infinite or NaN
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            q[e] = 0;
-    } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            q[e] = quant(y[e], s);
-    }
+    quants<VEC>(y, s, q);
     if constexpr (VEC == 8) {
         unsigned u[2];
 #pragma unroll
@@ -451,10 +469,10 @@ cudaError_t launch_ring(K kernel, const A &a, const RingPlan &p, int64_t grid, c
 // arrays.  The units come asynchronously, two rows ahead, the single elements
 // in a register, one row ahead.  bf16, us, element by element from memory / so:
 // x + residual 16384 x 1003 59 / 37, 8192 x 4095 185 / 62; in 8 bits (x alone)
-// 69 / 39, 221 / 76; backward 76 / 48, 197 / 89.  Columns per thread: 16 from 512
+// 69 / 32, 221 / 62; backward 76 / 48, 197 / 89.  Columns per thread: 16 from 512
 // columns on (8192 x 4095 x + residual 62 us, 82 with 8), 8 for shorter rows
 // (65536 x 130 41 us, 47 with 16) and for 8 bits, whose second reduction wants
-// the warps (76 us, 92 with 16).
+// the warps (with a residual 93 us, 95 with 16; without one 62 and 58).
 template <typename T>
 struct RowCut {
     static constexpr int VE = 16 / sizeof(T);
@@ -601,11 +619,12 @@ __global__ void __launch_bounds__(NV == 16 ? 512 : 1024, 1) k_rmsnorm_shifted(No
             for (int k = 0; k < NV; ++k)
                 top = max_nan(top, fabsf(s[k]));
             const RowScale sc = row_scale(cta_join<true>(top, part[par][1]));
-            const bool zero = !sc.divide && sc.inv == 0.f;
+            unsigned q[NV];
+            quants<NV>(s, sc, q);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
                 if (k * nt + tid < D)
-                    reinterpret_cast<int8_t *>(ybuf + ys)[k * nt + tid] = zero ? 0 : (int8_t)(quant(s[k], sc) & 0xff);
+                    reinterpret_cast<int8_t *>(ybuf + ys)[k * nt + tid] = (int8_t)(q[k] & 0xff);
             if (tid == 0)
                 a.scales[row] = sc.scale;
         } else {
@@ -657,13 +676,17 @@ cudaError_t launch_shifted(K kernel, const A &a, const ShiftPlan &p, int64_t gri
 // a few tokens is all latency), four otherwise: two or eight were 10 to 60 %
 // slower on 65536 x 1024 to 8192 x 8192.  Rows off the 16-byte boundaries are
 // taken element by element.
-//   The ring where it pays, us for 67 M elements, ring / one row at a time:
-//   8 bits of x + residual  8192 columns 76 / 84, 4096 75 / 85, 1024 100 / 75;
-//   x alone in its type     8192 46 / 49, 4096 46 / 46, 1024 47 / 42;
-//   x + residual            8192 88 / 79 (all bf16): the simple form is at
-//                           the copy bandwidth already.
-//   Rows without a norm need few registers: six CTAs of 256 threads per SM (45
-// us for 8192 x 8192 bf16, 49 with four).
+//   The ring where it pays, us, ring / one row at a time:
+//   x alone in its type     8192 x 8192 bf16 46 / 49, 16384 x 4096 46 / 46,
+//                           65536 x 1024 47 / 42;
+//   x + residual            8192 x 8192 88 / 79: the simple form is at the copy
+//                           bandwidth already;
+//   8 bits of x + residual  all bf16 8000 x 12288 105 / 131, 2048 x 8192 20.5 /
+//                           24.0, 4095 x 8192 41.1 / 42.4, but 6000 x 8192 60.7 /
+//                           59.1 and 16384 x 4096 82.8 / 74.6; with a residual
+//                           in fp32 8192 x 8192 128 / 110, 8000 x 12288 184 / 169.
+//   Rows without a norm need few registers: six CTAs of 256 threads per SM (40
+// us for 8192 x 8192 bf16, 41 with four).
 template <typename XT, typename RT, bool RES, bool NORM, int OUT>
 cudaError_t pick_norm(const NormArgs &a, bool grouped8, cudaStream_t stream)
 {
@@ -673,10 +696,12 @@ cudaError_t pick_norm(const NormArgs &a, bool grouped8, cudaStream_t stream)
         if constexpr (!NORM) {
             if (a.D <= 8192)
                 return go_norm<XT, RT, RES, NORM, OUT, 8, 4, 256, 6>(a, stream);
-        } else if constexpr (OUT == kOutInt || !RES) {
+        } else if constexpr (!RES || (OUT == kOutInt && sizeof(RT) == 2)) {
             const RingPlan p = ring_plan(a.D, a.D * (int64_t)(sizeof(XT) + (RES ? sizeof(RT) : 0)));
             const int64_t grid = (int64_t)kSms * p.per_sm;
-            if (p.on && a.D > (OUT == kOutInt ? 1024 : 4096) && a.T >= 2 * grid)
+            const bool pays = !RES ? a.D > (OUT == kOutInt ? 1024 : 4096)
+                                   : a.D > 8192 || (a.D > 4096 && a.T <= 14 * grid);
+            if (p.on && pays && a.T >= 2 * grid)
                 return p.block <= 256
                            ? launch_ring(k_rmsnorm_ring<XT, RT, RES, OUT, 256, 2>, a, p, grid, stream)
                            : launch_ring(k_rmsnorm_ring<XT, RT, RES, OUT, 512, 1>, a, p, grid, stream);

@@ -1,0 +1,68 @@
+"""The operators where their kernels' forms differ: codes next to a tie, rows
+masked far below zero, and the forms that only longer calls take.  References and
+bounds as in test_ops_gpu.
+"""
+import pytest
+import torch
+from test_ops_gpu import BF, F32, gen, randn
+
+from paper_2607_01455_gb300 import Ops
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops(cuda_device):
+    return Ops(cuda_device)
+
+
+# ---- 8-bit codes: the fp32 quotient y / scale, rounded to nearest even ----
+
+def over_127(x):
+    """x / 127, rounded once (by a Python number torch multiplies by its reciprocal)."""
+    return x / torch.full_like(x, 127.0)
+
+
+def near_ties(g, D):
+    """D values of a row, the largest in front: the others lie within two
+    steps of fp32 around (m + 1/2) scale."""
+    top = (1.0 + torch.rand(1, generator=g, device="cuda")).float()
+    scale = top / 127
+    m = torch.randint(-126, 126, (D - 1,), generator=g, device="cuda")
+    y = ((m + 0.5).double() * scale.double()).float()
+    by = torch.randint(-2, 3, (D - 1,), generator=g, device="cuda")
+    for step in (1, 2):
+        y = torch.where(by >= step, torch.nextafter(y, y + 1), y)
+        y = torch.where(by <= -step, torch.nextafter(y, y - 1), y)
+    return torch.cat([top, y])
+
+
+@pytest.mark.parametrize("T,D,pad", [(3, 1003, 0), (1, 4096, 0), (400, 512, 0), (200, 1003, 0), (40, 8200, 0),
+                                     (5, 8193, 0), (33, 96, 5)])
+def test_codes_next_to_a_tie(ops, T, D, pad):
+    g = gen(T + D)
+    x = torch.zeros(T, D + pad, device="cuda")[:, :D]
+    for t in range(T):
+        x[t] = near_ties(g, D) * 2.0 ** (t % 40 - 20)
+    q, scales = ops.quantize_rows(x)
+    assert torch.equal(scales, over_127(x.abs().amax(1)))
+    assert torch.equal(q, torch.round(x / scales[:, None]).to(torch.int8))
+
+
+@pytest.mark.parametrize("t", [BF, F32])
+def test_codes_of_a_table(ops, t):
+    x = (randn(gen(1), 5000, 4096) * 0.02).to(t)
+    q, scales = ops.quantize_rows(x)
+    assert torch.equal(q, torch.round(x.float() / scales[:, None]).to(torch.int8))
+
+
+@pytest.mark.parametrize("T,D", [(2, 256), (3, 1024), (300, 4096), (2500, 4096), (9, 16384)])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_codes_of_the_norm_next_to_a_tie(ops, T, D, offset):
+    """Rows of ones of either sign: with eps = 0 the norm is exactly 1 and y the gain with their signs."""
+    g = gen(D)
+    gain = near_ties(g, D)
+    x = torch.randint(0, 2, (T, D + offset), generator=g, device="cuda").float()[:, offset:] * 2 - 1
+    q, scales, _ = ops.rmsnorm_quant(x, gain, eps=0.0)
+    assert torch.equal(scales, over_127(gain[:1]).expand(T))
+    assert torch.equal(q, torch.round(x * gain / scales[:, None]).to(torch.int8))
