@@ -536,7 +536,9 @@ k_loss_rows(LossArgs a)
             a.nll[t] = 0.f;
         const float g = w * inv_n;
         const float gs = __fdividef(g, ms.s);  // a sum is between 1 and 2^18: within two ulps
-        const float f = live ? exp_of(m0 - m) * gs : 0.f;
+        // by the thread's own maximum, not m0: where it saw nothing but -inf, its values
+        // are 0 and so is the factor, which 0 - m could make infinite
+        const float f = live ? exp_of(mt - m) * gs : 0.f;
         // the target's loss and gradient, by the thread that has it among its logits
         const int yu = on ? (int)y - c.head - c.u0 * VE : -1;  // its place among this slice's logits
         const bool mine = yu >= 0 && yu < c.n * VE && yu / VE % nt == tid;

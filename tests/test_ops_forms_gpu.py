@@ -2,11 +2,14 @@
 masked far below zero, and the forms that only longer calls take.  References and
 bounds as in test_ops_gpu.
 """
+import math
+
 import pytest
 import torch
-from test_ops_gpu import BF, F32, gen, randn
+from test_ops_gpu import BF, F32, check_loss, gen, randn, rows
 
 from paper_2607_01455_gb300 import Ops
+from paper_2607_01455_gb300 import ember as E
 
 pytestmark = pytest.mark.gpu
 
@@ -66,3 +69,37 @@ def test_codes_of_the_norm_next_to_a_tie(ops, T, D, offset):
     q, scales, _ = ops.rmsnorm_quant(x, gain, eps=0.0)
     assert torch.equal(scales, over_127(gain[:1]).expand(T))
     assert torch.equal(q, torch.round(x * gain / scales[:, None]).to(torch.int8))
+
+
+# ---- masked entries of rows far below zero ----
+
+def below(g, T, V, t, base, pad=0, offset=0):
+    z = rows(g, T, V, t, pad, offset)
+    z += base
+    z[:, V // 2:] = -math.inf
+    z[1::3, :V // 4] = -math.inf
+    return z, torch.randint(V // 4, V // 2, (T,), generator=g, device="cuda")
+
+
+@pytest.mark.parametrize("T,V", [(6, 40), (6, 1003), (8, 50257), (4, 262144), (3, 300000), (1030, 1003), (1100, 5003),
+                                 (1030, 30000), (1030, 50257), (3, 600001)])
+@pytest.mark.parametrize("t", [BF, F32])
+@pytest.mark.parametrize("base", [-100.0, -1e4, -1e30])
+def test_masks_of_rows_far_below_zero(ops, T, V, t, base):
+    """Where all that a thread holds of a row is masked out, the row's maximum
+    may still be any number: the masked gradients are zero, the others those of the row."""
+    z, y = below(gen(V), T, V, t, base)
+    for w in (None, torch.full((T,), 1e6, device="cuda")):
+        loss, nll, d = check_loss(ops, z, y, w)
+        assert (d[:, V // 2:] == 0).all() and (d[1::3, :V // 4] == 0).all()
+    assert ops.device_status() == E.EMBER_OK
+
+
+@pytest.mark.parametrize("V", [40, 50257])
+def test_a_nan_beside_masks_far_below_zero(ops, V):
+    """A NaN still reaches the whole of its row, whichever thread sees it, and no other row."""
+    z, y = below(gen(V), 5, V, F32, -200.0)
+    z[0, V - 1] = z[1, V // 4] = z[2, 0] = math.nan
+    loss, nll, d = ops.softmax_loss(z, y)
+    assert torch.isnan(nll[:3]).all() and torch.isnan(d[:3]).all() and torch.isnan(loss)
+    assert torch.isfinite(nll[3:]).all() and torch.isfinite(d[3:]).all()
