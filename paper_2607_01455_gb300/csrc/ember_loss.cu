@@ -389,8 +389,10 @@ k_loss_rows(LossArgs a)
     };
     bool failed = false;  // a wait of this thread gave up
     bool met = false;     // the first cluster barrier is behind this CTA
+    // A try may suspend its thread for longer than these copies take: a limit
+    // below a microsecond is kept by looking once.
     auto wait = [&](uint32_t b, uint32_t parity) {
-        if (!failed && !tc::mbar_spin(b, parity, abort, a.wait_ns)) {
+        if (!failed && !tc::mbar_look(b, parity) && (a.wait_ns < 1000 || !tc::mbar_spin(b, parity, abort, a.wait_ns))) {
             failed = true;
             atomicOr(a.status, kFlagTimeout);
             *abort = 1;
@@ -580,15 +582,8 @@ k_loss_rows(LossArgs a)
     const bool gave_up = __syncthreads_or(failed);
     if (C > 1 && !met)
         tc::cluster_wait();
-    if (gave_up && tid == 0) {
-        // what is in flight has landed before the CTA ends: the copy it started
-        // last, and the other CTAs' pairs (they take about a microsecond)
-        if (started)
-            tc::mbar_wait_final(bar, (started - 1u) & 1u);
-        const uint64_t t0 = dev::now_ns();
-        while (dev::now_ns() - t0 < 100000)
-            ;
-    }
+    if (gave_up && tid == 0 && started)  // the copy it started last has landed before the CTA ends
+        tc::mbar_wait_final(bar, (started - 1u) & 1u);
     // few tokens: the last CTA to come here adds the losses up
     if constexpr (HERE) {
         __shared__ double dpart[16];
@@ -601,6 +596,13 @@ k_loss_rows(LossArgs a)
     }
     if (C > 1)
         tc::cluster_sync();  // no CTA leaves while another may still send to it
+    // What a CTA that gave up did not wait for may still be on its way to it; all of
+    // it has been sent by now and takes about a microsecond.
+    if (gave_up && tid == 0) {
+        const uint64_t t0 = dev::now_ns();
+        while (dev::now_ns() - t0 < 100000)
+            ;
+    }
 }
 
 // Threads per CTA and CTAs per row for rows of V logits; C = 0 where a row

@@ -103,3 +103,32 @@ def test_a_nan_beside_masks_far_below_zero(ops, V):
     loss, nll, d = ops.softmax_loss(z, y)
     assert torch.isnan(nll[:3]).all() and torch.isnan(d[:3]).all() and torch.isnan(loss)
     assert torch.isfinite(nll[3:]).all() and torch.isfinite(d[3:]).all()
+
+
+# ---- waits of the loss that run out ----
+
+@pytest.mark.parametrize("T,V", [(60, 500000), (1100, 500000), (1100, 60000), (40, 20000)])
+@pytest.mark.parametrize("ignored", [0, 2])
+def test_a_wait_of_the_loss_that_gives_up_is_reported(cuda_device, T, V, ignored):
+    """Rows of two and more CTAs: with a limit of 1 ns the wait for the first
+    copy gives up or, where there is none to wait for, that for the other CTAs'
+    sums, which have only just been sent.  Each call returns, the status says so,
+    and later calls give the bits that earlier ones gave."""
+    ops, g = Ops(cuda_device), gen(13)
+    z, y = rows(g, T, V, BF), torch.randint(0, V, (T,), generator=g, device="cuda")
+    if ignored:
+        y[::ignored] = -100
+    want = [t.clone() for t in ops.softmax_loss(z, y)]
+    assert ops.device_status() == E.EMBER_OK
+    try:
+        ops.set_wait_limit_ns(1)
+        for _ in range(10):
+            ops.softmax_loss(z, y)
+            assert ops.device_status() == E.EMBER_ERR_TIMEOUT
+            assert ops.device_status() == E.EMBER_OK  # cleared by the reading
+    finally:
+        ops.set_wait_limit_ns(0)
+    for _ in range(2):
+        for a, b in zip(ops.softmax_loss(z, y), want):
+            assert torch.equal(a, b)
+        assert ops.device_status() == E.EMBER_OK
