@@ -10,13 +10,15 @@
 // workspace's address and size and the status block's address, then the
 // operator's arguments; it returns the outputs, a status (an int) if libember
 // refused the call, or None where the arguments are not the common case (other
-// types, devices or strides, a workspace that is too small).  ops.py then
+// types, devices or strides, a device that is not the current one, a workspace
+// that is too small).  ops.py then
 // takes its own path, which grows the workspace or names what is wrong.
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <c10/util/Exception.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -389,6 +391,11 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
         return nullptr;
     }
     try {
+        // libember launches on the current device: another one's call is left to
+        // the module, which makes it current (about 0.03 us here, 0.25 there)
+        c10::DeviceIndex current;
+        if (c10::cuda::GetDevice(&current) != cudaSuccess || current != PyLong_AsLongLong(args[0]))
+            Py_RETURN_NONE;
         return F(args);
     } catch (const c10::OutOfMemoryError &) {
         Py_RETURN_NONE;  // before the launch; the module's own path raises torch's exception

@@ -28,9 +28,10 @@ from array import array
 import torch
 
 from .ember import (EMBER_BF16, EMBER_ERR_DTYPE, EMBER_ERR_INVALID_ARG, EMBER_F32, EMBER_I32, EMBER_I64, EMBER_OK,
-                    EmberError, _check, _current_stream, lib, ops_binding)
+                    EmberError, _check, lib, ops_binding)
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 
 _TYPES = {torch.bfloat16: EMBER_BF16, torch.float32: EMBER_F32}
 _IDS = {torch.int32: EMBER_I32, torch.int64: EMBER_I64}
@@ -46,7 +47,8 @@ class _Refused(EmberError, ValueError):
 class Ops:
     """The operators' workspace and status block on one device, for use
     on one stream (calls on different streams share the workspace: give each
-    stream its own object).  Before a graph capture, make each call once."""
+    stream its own object).  The device need not be the current one.  Before a
+    graph capture, make each call once."""
 
     def __init__(self, device="cuda"):
         dev = torch.device(device)
@@ -118,10 +120,16 @@ class Ops:
             self._status = torch.zeros(4, dtype=torch.int32, device=self.device)  # EMBER_STATUS_BYTES
         return self._status.data_ptr()
 
-    def _on(self, stream):
-        """A context in which torch allocates from the stream that the call runs on."""
+    def _on(self, stream=None):
+        """A context in which this object's device is the current one (libember
+        launches there, and the default stream's handle means that of the
+        current device) and torch allocates from the stream that the call runs on."""
+        if stream is None:
+            return torch.cuda.device(self.device)
         if isinstance(stream, int):
             stream = torch.cuda.ExternalStream(stream, device=self.device)
+        elif stream.device != self.device:
+            raise _Refused("stream", f"it is on {stream.device}, not on {self.device}")
         return torch.cuda.stream(stream)
 
     # ---- the norm ----
@@ -147,6 +155,9 @@ class Ops:
         r = self._fast.rmsnorm(self._index, x, gain, residual, eps, out, residual_out)
         if r is not None:
             return r if r.__class__ is not int else _check(r, w)
+        if _current_device() != self._index:
+            with self._on():
+                return self.rmsnorm(x, gain, residual, eps, out, residual_out)
         px, ldx = self._matrix(w, "x", x, _TYPES)
         shape, xt = x.shape, x.dtype
         T, D = shape
@@ -176,6 +187,9 @@ class Ops:
         r = self._fast.rmsnorm_quant(self._index, x, gain, residual, eps, residual_out)
         if r is not None:
             return r if r.__class__ is not int else _check(r, w)
+        if _current_device() != self._index:
+            with self._on():
+                return self.rmsnorm_quant(x, gain, residual, eps, residual_out)
         px, ldx = self._matrix(w, "x", x, _TYPES)
         T, D = x.shape
         pg, gt = self._gain(w, gain, D)
@@ -201,6 +215,9 @@ class Ops:
         r = self._fast.rmsnorm_backward(self._index, self._at, self._bytes, dy, h, gain, eps, dres, out)
         if r is not None:
             return r if r.__class__ is not int else _check(r, w)
+        if _current_device() != self._index:
+            with self._on():
+                return self.rmsnorm_backward(dy, h, gain, eps, dres, out)
         ph, ldh = self._matrix(w, "h", h, _TYPES)
         shape, same = h.shape, (h.dtype,)
         T, D = shape
@@ -219,7 +236,7 @@ class Ops:
     def quantize_rows(self, x, stream=None):
         """(q, scales) of a matrix: scales = max |x| / 127 over each row, q = x
         / scales rounded to nearest even.  Rows of q start on 16 bytes."""
-        if stream is not None:
+        if stream is not None or _current_device() != self._index:
             with self._on(stream):
                 return self.quantize_rows(x)
         w = "quantize_rows"
@@ -239,6 +256,9 @@ class Ops:
         r = self._fast.dequantize_rows(self._index, q, scales, _TYPES.get(dtype, -1), out)
         if r is not None:
             return r if r.__class__ is not int else _check(r, w)
+        if _current_device() != self._index:
+            with self._on():
+                return self.dequantize_rows(q, scales, dtype, out)
         pq, ldq = self._matrix(w, "q", q, (torch.int8,))
         T, D = q.shape
         ps = self._vector(w, "scales", scales, T, (torch.float32,))
@@ -259,6 +279,9 @@ class Ops:
                                     _TYPES.get(dtype, -1), out)
         if r is not None:
             return r if r.__class__ is not int else _check(r, w)
+        if _current_device() != self._index:
+            with self._on():
+                return self.matmul_quant(xq, xs, wq, ws, dtype, out)
         px, ldx = self._matrix(w, "xq", xq, (torch.int8,))
         T, K = xq.shape
         pw, ldw = self._matrix(w, "wq", wq, (torch.int8,))
@@ -296,6 +319,9 @@ class Ops:
                                     ignore_index, reduction == "mean", _TYPES.get(dt, -2) if grad else -1, out)
         if r is not None:
             return r if r.__class__ is not int else _check(r, w)
+        if _current_device() != self._index:
+            with self._on():
+                return self.softmax_loss(logits, targets, weights, ignore_index, reduction, grad, grad_dtype, out)
         pz, ldz = self._matrix(w, "logits", logits, _TYPES)
         T, V = logits.shape
         py = self._vector(w, "targets", targets, T, _IDS)
@@ -357,6 +383,9 @@ class Ops:
         r = self._fast.grad_norm(self._index, self._at, self._bytes, tensors)
         if r is not None:
             return r if r.__class__ is not int else _check(r, w)
+        if _current_device() != self._index:
+            with self._on():
+                return self.grad_norm(tensors)
         ptrs, _, numel, types = self._list(w, tensors, None)
         norm = self._new((), torch.float32)
         n = len(tensors)
@@ -377,6 +406,9 @@ class Ops:
         r = self._fast.clip_grads(self._index, self._at, self._bytes, tensors, max_norm, eps, out)
         if r is not None:
             return r if r.__class__ is not int else _check(r, w)
+        if _current_device() != self._index:
+            with self._on():
+                return self.clip_grads(tensors, max_norm, out, eps)
         ptrs, outs, numel, types = self._list(w, tensors, out)
         norm = self._new((), torch.float32)
         n = len(tensors)
@@ -389,8 +421,11 @@ class Ops:
     def device_status(self, stream=None):
         """Synchronises; returns (and clears) the sticky status: EMBER_OK,
         EMBER_ERR_ID_OUT_OF_RANGE (a target) or EMBER_ERR_TIMEOUT."""
-        return self._lib.ember_status_read(self._status_word(),
-                                           _current_stream() if stream is None else getattr(stream, "cuda_stream", stream))
+        if _current_device() != self._index:
+            with self._on():
+                return self.device_status(stream)
+        at = _raw_stream(self._index) if stream is None else getattr(stream, "cuda_stream", stream)
+        return self._lib.ember_status_read(self._status_word(), at)
 
     def set_wait_limit_ns(self, ns):
         """Limit of the bounded waits inside the kernels, for every call of this
