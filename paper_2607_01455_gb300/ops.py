@@ -127,7 +127,9 @@ class Ops:
         if stream is None:
             return torch.cuda.device(self.device)
         if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=self.device)
+            # the handle 0 is the default stream; torch would take it for none and give a new one
+            stream = (torch.cuda.ExternalStream(stream, device=self.device) if stream
+                      else torch.cuda.default_stream(self.device))
         elif stream.device != self.device:
             raise _Refused("stream", f"it is on {stream.device}, not on {self.device}")
         return torch.cuda.stream(stream)

@@ -92,3 +92,11 @@ def test_a_stream_of_another_device_is_refused(monkeypatch, name):
     with pytest.raises(ValueError, match="stream"):
         getattr(m.ops, name)(*CALLS[name], stream=s)
     assert m.seen == [] and m.current == 0
+
+
+def test_the_handle_0_is_the_default_stream(monkeypatch):
+    m = Machine(monkeypatch)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda d: types.SimpleNamespace(device=d, cuda_stream=0))
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda p, device: pytest.fail("no stream has this handle"))
+    m.ops.rmsnorm(X, None, stream=0)
+    assert m.seen[0][1] == 1 and m.current == 0

@@ -132,3 +132,29 @@ def test_a_wait_of_the_loss_that_gives_up_is_reported(cuda_device, T, V, ignored
         for a, b in zip(ops.softmax_loss(z, y), want):
             assert torch.equal(a, b)
         assert ops.device_status() == E.EMBER_OK
+
+
+# ---- streams by their handle ----
+
+def test_streams_by_their_handle(ops):
+    """The handle 0 is the default stream, any other the stream that has it."""
+    side = torch.cuda.Stream()
+    for on in (None, side):
+        with torch.cuda.stream(on):
+            for s in (torch.cuda.default_stream(), side):
+                with ops._on(s.cuda_stream):
+                    assert torch.cuda.current_stream().cuda_stream == s.cuda_stream
+
+
+def test_calls_on_the_handle_0_follow_the_default_stream(ops):
+    """Inputs written by long work on the default stream right before each call."""
+    x = torch.zeros(300, 1024, device="cuda")
+    big = torch.zeros(1 << 28, device="cuda")
+    ops.rmsnorm(x, None)
+    for k in range(1, 6):
+        big.add_(1.0)
+        x.fill_(float(k))
+        y, _ = ops.rmsnorm(x, None, eps=0.0, stream=0)
+        torch.cuda.synchronize()
+        assert (y == 1).all()
+        x.zero_()
