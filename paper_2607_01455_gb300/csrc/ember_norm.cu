@@ -1111,8 +1111,9 @@ struct BackPlan {
     int64_t parts;  // partial rows
 };
 
-// Long rows of whole groups go through the ring, rows off the boundaries through
-// shared memory with their shifts; the rest keeps one row in registers.
+// Rows of whole groups from 1024 columns on go through the ring where it fits,
+// rows off the boundaries through shared memory with their shifts; the rest keeps
+// one row in registers: up to 1023 columns, and those too wide for the other two.
 BackPlan back_plan(int64_t T, int64_t D, int esize, bool res, bool grouped8)
 {
     BackPlan p{};
@@ -1122,7 +1123,7 @@ BackPlan back_plan(int64_t T, int64_t D, int esize, bool res, bool grouped8)
     p.shift = shift_plan(D, (res ? 3 : 2) * row, row, true);
     p.shift.on = p.shift.on && !grouped8;
     p.vec = grouped8 ? 8 : 1;
-    p.nv = grouped8 ? (D <= 2048 ? 1 : D <= 8192 ? 2 : 4) : 32;
+    p.nv = grouped8 ? (D < 1024 ? 1 : 4) : 32;
     p.tpr = threads_per_row(D, p.vec, p.nv);
     p.block = p.tpr < kMinBlock ? kMinBlock : p.tpr;
     const int64_t rpc = p.ring.on || p.shift.on ? 1 : p.block / p.tpr;
@@ -1148,10 +1149,12 @@ cudaError_t launch_back(BackArgs a, const BackPlan &p, cudaStream_t stream)
     auto go = [&](auto kernel) { return launch_k(kernel, dim3(p.grid), dim3(p.block), 0, stream, true, a); };
     if (p.vec == 8) {
         if (p.nv == 1)
-            return go(k_rmsnorm_back<XT, RES, 8, 1, 256>);
-        if (p.nv == 2)
-            return go(k_rmsnorm_back<XT, RES, 8, 2, 512>);
-        return p.block <= 512 ? go(k_rmsnorm_back<XT, RES, 8, 4, 512>) : go(k_rmsnorm_back<XT, RES, 8, 4, 1024>);
+            return go(k_rmsnorm_back<XT, RES, 8, 1, 128>);
+        if constexpr (sizeof(XT) == 4) {  // bf16 rows of up to 16384 columns always fit the ring
+            if (p.block <= 512)
+                return go(k_rmsnorm_back<XT, RES, 8, 4, 512>);
+        }
+        return go(k_rmsnorm_back<XT, RES, 8, 4, 1024>);
     }
     return p.block <= 512 ? go(k_rmsnorm_back<XT, RES, 1, 32, 512>) : go(k_rmsnorm_back<XT, RES, 1, 32, 1024>);
 }
