@@ -6,7 +6,8 @@ import math
 
 import pytest
 import torch
-from test_ops_gpu import BF, F32, check_loss, gen, randn, rows
+from test_ops_gpu import (BACK_U, BF, F32, NORM_U, U, back64, check_loss, check_rows8, close, gen, norm64, out_u, randn,
+                          rows)
 
 from paper_2607_01455_gb300 import Ops
 from paper_2607_01455_gb300 import ember as E
@@ -158,3 +159,99 @@ def test_calls_on_the_handle_0_follow_the_default_stream(ops):
         torch.cuda.synchronize()
         assert (y == 1).all()
         x.zero_()
+
+
+# ---- forms that longer calls take ----
+
+TYPES = [(BF, None), (BF, BF), (BF, F32), (F32, None), (F32, BF), (F32, F32)]
+
+
+@pytest.mark.parametrize("T,D", [(2500, 1032), (1000, 4104), (700, 8192), (4400, 8192), (400, 8200),
+                                 (320, 12800), (310, 16384)])
+@pytest.mark.parametrize("xt,rt", TYPES)
+def test_long_calls_of_the_norm(ops, T, D, xt, rt):
+    """Rows of whole groups, each CTA taking several of them, with and without 8 bits."""
+    g = gen(T + D)
+    x = rows(g, T, D, xt)
+    res = None if rt is None else rows(g, T, D, rt, scale=2.0)
+    gain = 1 + 0.1 * randn(g, D)
+    s64, y64 = norm64(x, gain, res, 1e-6)
+    q, scales, h = ops.rmsnorm_quant(x, gain, residual=res)
+    check_rows8(q, scales, y64, NORM_U)
+    y, h2 = ops.rmsnorm(x, gain, residual=res)
+    close(y, y64, (NORM_U + out_u(xt)) * y64.abs(), "y")
+    if res is not None:
+        close(h, s64, (U + out_u(rt)) * s64.abs(), "h")
+        assert torch.equal(h, h2)
+    for a, b in zip(ops.rmsnorm_quant(x, gain, residual=res), (q, scales, h)):
+        assert (a is None and b is None) or torch.equal(a, b)
+    # in place
+    x2, r2 = x.clone(), None if res is None else res.clone()
+    ops.rmsnorm(x2, gain, residual=r2, out=x2, residual_out=r2)
+    assert torch.equal(x2, y) and (res is None or torch.equal(r2, h2))
+
+
+@pytest.mark.parametrize("T,D", [(15000, 33), (12000, 130), (5000, 1003), (2000, 4095), (400, 8191)])
+@pytest.mark.parametrize("xt,rt", TYPES)
+def test_long_calls_of_odd_rows(ops, T, D, xt, rt):
+    """Rows off the 16-byte boundaries, each CTA taking several of them."""
+    g = gen(T + D)
+    x = rows(g, T, D, xt)
+    res = None if rt is None else rows(g, T, D, rt, scale=2.0)
+    gain = 1 + 0.1 * randn(g, D)
+    s64, y64 = norm64(x, gain, res, 1e-6)
+    y, h = ops.rmsnorm(x, gain, residual=res)
+    close(y, y64, (NORM_U + out_u(xt)) * y64.abs(), "y")
+    q, scales, h2 = ops.rmsnorm_quant(x, gain, residual=res)
+    check_rows8(q, scales, y64, NORM_U)
+    if res is not None:
+        close(h, s64, (U + out_u(rt)) * s64.abs(), "h")
+        assert torch.equal(h, h2)
+    else:
+        q, scales = ops.quantize_rows(x)
+        assert torch.equal(q, torch.round(x.float() / scales[:, None]).to(torch.int8))
+    # rows at other places of the buffers, and in place
+    guard = torch.full((T, D + 3), 7.0, device="cuda", dtype=xt)
+    ops.rmsnorm(x, gain, residual=res, out=guard[:, 2:D + 2])
+    assert torch.equal(guard[:, 2:D + 2], y) and (guard[:, :2] == 7).all() and (guard[:, D + 2:] == 7).all()
+    x2, r2 = x.clone(), None if res is None else res.clone()
+    ops.rmsnorm(x2, gain, residual=r2, out=x2, residual_out=r2)
+    assert torch.equal(x2, y) and (res is None or torch.equal(r2, h))
+
+
+@pytest.mark.parametrize("T,D", [(2000, 256), (1500, 1024), (1000, 4104), (700, 8192), (400, 8200), (320, 10000),
+                                 (310, 16384), (200, 20000), (15000, 33), (5000, 1003), (2000, 4095), (400, 8191), (300, 9001),
+                                 (200, 16401)])
+@pytest.mark.parametrize("t,with_dres", [(BF, True), (BF, False), (F32, True), (F32, False)])
+def test_long_calls_of_the_norm_backward(ops, T, D, t, with_dres):
+    g = gen(T + D)
+    h, dy = rows(g, T, D, t, scale=2.0), rows(g, T, D, t, scale=1e-3)
+    dres = rows(g, T, D, t, scale=1e-3) if with_dres else None
+    gain = 1 + 0.1 * randn(g, D)
+    dx, dgain = ops.rmsnorm_backward(dy, h, gain, dres=dres)
+    dx64, mag, dg64, dgmag = back64(dy, h, gain, 1e-6, dres)
+    close(dx, dx64, BACK_U * mag + out_u(t) * dx64.abs(), "dx")
+    close(dgain, dg64, (T + 8) * U * dgmag + NORM_U * dgmag, "dgain")
+    d2 = dy.clone()
+    again = ops.rmsnorm_backward(d2, h, gain, dres=dres, out=d2)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dgain)
+
+
+@pytest.mark.parametrize("T,V", [(1500, 777), (1100, 30000), (1100, 50257), (1030, 64000), (1030, 128256), (1030, 270000)])
+@pytest.mark.parametrize("zt,dt", [(BF, BF), (BF, F32), (F32, F32), (F32, BF)])
+def test_long_calls_of_the_loss(ops, T, V, zt, dt):
+    """More tokens than one launch takes, by rows of each number of threads and CTAs."""
+    g = gen(T + V)
+    z = rows(g, T, V, zt, scale=3.0)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    y[5::11] = -100
+    w = randn(g, T)
+    loss, nll, d = check_loss(ops, z, y, w, dtype=dt)
+    assert (nll[5::11] == 0).all() and (d[5::11] == 0).all()
+    l2, n2, none = ops.softmax_loss(z, y, weights=w, grad=False)
+    assert none is None and torch.equal(l2, loss) and torch.equal(n2, nll)
+    if zt == dt:
+        z2 = z.clone()
+        l2, n2, d2 = ops.softmax_loss(z2, y, weights=w, out=z2)
+        assert torch.equal(l2, loss) and torch.equal(n2, nll) and torch.equal(d2, d)
+    assert ops.device_status() == E.EMBER_OK
