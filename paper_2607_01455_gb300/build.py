@@ -19,7 +19,6 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB_DIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIB_DIR, "libember.so")
-BINDING = os.path.join(LIB_DIR, "_ops_binding.so")
 
 NVCC = os.environ.get("NVCC", "nvcc")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -60,25 +59,33 @@ def build_library(force: bool = False, verbose_ptxas: bool = False) -> str:
     return LIB
 
 
-def build_binding(force: bool = False) -> str:
-    """Build the operators' binding unless it is newer than its source."""
-    src = os.path.join(CSRC, "ops_binding.cpp")
-    if (not force and os.path.exists(BINDING)
-            and os.path.getmtime(BINDING) >= max(os.path.getmtime(p) for p in (src, os.path.join(INCLUDE, "ember.h")))):
-        return BINDING
+def binding_path() -> str:
+    """Where the operators' binding for this interpreter and the torch at hand
+    belongs: it fits the libraries of the torch that it was built against alone."""
     import torch
+    return os.path.join(LIB_DIR, f"_ops_binding.{sysconfig.get_config_var('SOABI')}.torch-{torch.__version__}.so")
+
+
+def build_binding(force: bool = False) -> str:
+    """Build the operators' binding for the torch at hand unless it is there and newer than its source."""
+    import torch
+    binding = binding_path()
+    src = os.path.join(CSRC, "ops_binding.cpp")
+    if (not force and os.path.exists(binding)
+            and os.path.getmtime(binding) >= max(os.path.getmtime(p) for p in (src, os.path.join(INCLUDE, "ember.h")))):
+        return binding
     os.makedirs(LIB_DIR, exist_ok=True)
     home = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which(NVCC) or "/usr/local/cuda/bin/nvcc")))
     dirs = [INCLUDE, sysconfig.get_paths()["include"], os.path.join(home, "include"),
             os.path.join(home, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include")]
     libs = os.path.join(home, "lib")
-    tmp = BINDING + f".tmp{os.getpid()}"
+    tmp = binding + f".tmp{os.getpid()}"
     subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
                     *(a for d in dirs for a in ("-I", d)), src, "-o", tmp, "-L", libs, "-lc10", "-lc10_cuda",
                     "-ltorch_cpu", "-ltorch", "-ltorch_python", f"-Wl,-rpath,{libs}"], check=True)
-    os.replace(tmp, BINDING)
-    return BINDING
+    os.replace(tmp, binding)
+    return binding
 
 
 if __name__ == "__main__":

@@ -12,7 +12,6 @@ import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_lib", "libember.so")
-BINDING_PATH = os.path.join(_HERE, "_lib", "_ops_binding.so")
 
 EMBER_OK = 0
 EMBER_ERR_INVALID_ARG = 1
@@ -142,16 +141,17 @@ _binding = None
 
 def ops_binding():
     """The compiled calls of the operators on torch tensors, bound to libember;
-    raises if they have not been built."""
+    raises if they have not been built for the torch at hand."""
     global _binding
     if _binding is None:
         import importlib.util
 
-        import torch  # noqa: F401  (its libraries have to be loaded first)
+        from .build import binding_path
+        path = binding_path()  # imports torch, whose libraries have to be loaded first
         L = lib()
-        if not os.path.exists(BINDING_PATH):
-            raise RuntimeError(f"{BINDING_PATH} is missing: build it with __graft_entry__.build()")
-        spec = importlib.util.spec_from_file_location("_ops_binding", BINDING_PATH)
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with __graft_entry__.build()")
+        spec = importlib.util.spec_from_file_location("_ops_binding", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         module.bind(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in _BOUND))

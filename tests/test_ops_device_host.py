@@ -100,3 +100,15 @@ def test_the_handle_0_is_the_default_stream(monkeypatch):
     monkeypatch.setattr(torch.cuda, "ExternalStream", lambda p, device: pytest.fail("no stream has this handle"))
     m.ops.rmsnorm(X, None, stream=0)
     assert m.seen[0][1] == 1 and m.current == 0
+
+
+def test_the_binding_belongs_to_the_torch_at_hand(monkeypatch):
+    """One that was built for another torch is not loaded, and the message says what to do."""
+    from paper_2607_01455_gb300.build import binding_path, build_binding
+    path = build_binding()
+    assert path == binding_path() and torch.__version__ in path
+    assert E.ops_binding() is E.ops_binding()
+    monkeypatch.setattr(E, "_binding", None)
+    monkeypatch.setattr(torch, "__version__", "0.1")
+    with pytest.raises(RuntimeError, match="torch-0.1.so is missing: build"):
+        E.ops_binding()
