@@ -388,7 +388,9 @@ ember_status ember_set_ops_wait_limit(uint64_t ns);
  *   gain:     D values of gtype, or NULL for ones.
  *   eps >= 0, finite.  D <= 32768 (EMBER_ERR_UNSUPPORTED).  T = 0 does
  * nothing.  The squares are summed in fp32: values beyond about 1e19 give
- * an infinite mean and y = 0. */
+ * an infinite mean and y = 0, and an eps below 1e-37 does not stand in for the
+ * squares of rows of values below about 1e-19, which lose bits or vanish (the
+ * same holds of the gradients). */
 ember_status ember_rmsnorm(const void *x, int64_t ldx, ember_wdtype xtype,
                            const void *residual, int64_t ldr, ember_wdtype rtype,
                            const void *gain, ember_wdtype gtype, int64_t T, int64_t D, float eps,
@@ -430,6 +432,10 @@ ember_status ember_rmsnorm_backward(const void *dy, int64_t lddy, const void *h,
  *   out[t][v] = xs[t] ws[v] sum_k xq[t][k] wq[v][k]
  *   xq: T x K int8 with xs (T), wq: V x K int8 with ws (V); any values in
  *   [-128, 127].  out: T x V of otype, written.  K <= 32768.
+ * The sum is the integer as long as sum_k |xq wq| < 2^24 (always for K <= 1024).
+ * Beyond that it is the integer, rounded to fp32, in calls that sum in integers
+ * (few tokens, small tables, tables off 16 bytes); on the tensor cores it loses
+ * up to 2^-22 sum_k |xq wq| per 16 products, so a row's bits may depend on T.
  * T = 0 does nothing.  workspace: ember_matmul_quant_workspace_bytes(T, V,
  * K).  status (not NULL): EMBER_ERR_TIMEOUT if a bounded wait gave up. */
 size_t ember_matmul_quant_workspace_bytes(int64_t T, int64_t V, int64_t K);

@@ -36,7 +36,7 @@ template <int CAP>
 struct TensorList {
     const void *in[CAP];
     void *out[CAP];
-    int64_t n[CAP];            // elements, the top bit set for bf16
+    int64_t n[CAP];            // elements, with kBf16Bit set for bf16
     unsigned start[CAP + 1];   // first chunk of each tensor
     int count;
 };
@@ -67,7 +67,9 @@ __device__ __forceinline__ int tensor_of(const TensorList<CAP> &l, unsigned c)
 }
 
 // Sum of squares of N values: in 32 bits, in four chains, or nothing and
-// `wide` set where it must be done in 64.  Zeros need no more.
+// `wide` set where it must be done in 64.  A sum of zero is among those: zeros
+// and values whose squares vanish look alike in it, so groups of nothing but
+// zeros are read a second time too (right, but slower than others).
 template <int N>
 __device__ __forceinline__ double squares(const float (&v)[N], bool &wide)
 {
@@ -129,7 +131,7 @@ __device__ __forceinline__ double chunk_squares(const T *p, int64_t n, unsigned 
     }
     bool wide;
     double s = squares<NG * 8>(v, wide);
-    if (wide)  // read again: it is rare, and the values need not be kept for it
+    if (wide)  // read again, so that the values need not be kept for it
         for (int k = 0; k < NG; ++k) {
             const int64_t g = g0 + k * kClipThreads + threadIdx.x;
             for (int e = 0; g < ngroups && e < 8; ++e) {

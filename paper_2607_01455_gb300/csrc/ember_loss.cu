@@ -14,7 +14,7 @@
 // A row of up to 524288 logits is spread over a cluster of up to 16 CTAs and
 // stays in their registers between the statistics and the gradient; the CTAs
 // exchange one pair each through distributed shared memory.  4096 x 128256 bf16:
-// 342 us, 6.15 TB/s, 0.91 of the copy bandwidth (from 1052 us reading each row
+// 344 us, 6.12 TB/s, 0.90 of the copy bandwidth (from 1052 us reading each row
 // twice); what is left is latency: 24 warps per SM of 64 logits a thread.
 #include <atomic>
 
@@ -537,7 +537,7 @@ k_loss_rows(LossArgs a)
         if (!on && rank == 0 && tid == 0)
             a.nll[t] = 0.f;
         const float g = w * inv_n;
-        const float gs = __fdividef(g, ms.s);  // a sum is between 1 and 2^18: within two ulps
+        const float gs = __fdividef(g, ms.s);  // a sum is between 1 and 2^19: within two ulps
         // by the thread's own maximum, not m0: where it saw nothing but -inf, its values
         // are 0 and so is the factor, which 0 - m could make infinite
         const float f = live ? exp_of(mt - m) * gs : 0.f;

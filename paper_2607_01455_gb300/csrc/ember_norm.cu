@@ -53,9 +53,9 @@ __device__ __forceinline__ float row_reduce(float v, float *part, int tpr)
     return r;
 }
 
-// q = y / scale rounded to fp32 and then to nearest even, |q| <= 127.  A row of zeros has the
-// scale 0 and zeros; a row with an infinity or a NaN has the scale NaN and
-// zeros, so that what is formed from it is NaN throughout.
+// q = y / scale rounded to fp32 and then to nearest even, |q| <= 127.  A row of
+// zeros has the scale 0 and zeros; a row with an infinity or a NaN has the
+// scale NaN and zeros, so that what is formed from it is NaN throughout.
 struct RowScale {
     float scale, inv;
     bool divide;
@@ -78,10 +78,10 @@ __device__ __forceinline__ RowScale row_scale(float top)
 // The codes of VEC values, in the low bytes: adding 1.5 2^23 leaves a value
 // rounded to an integer, nearest even, in the low bits of the fp32 number.  The
 // quotient is y inv with one correction by its remainder (Markstein's division):
-// the remainder is exact, so what is rounded once more is the quotient to within
-// 2^-23 of its last place, and a value next to a tie falls to its side.  (By y inv
-// alone, which is off by up to 2^-17, one code in 10^5 differs.)  |quotient| is at most 127 (1 + 2^-23), so no bound is
-// needed there.
+// what is rounded once more is the quotient to within 2^-22 of its last place, so
+// a value next to a tie falls to its side.  (By y inv alone, which is off by up to
+// 2^-17, one code in 10^5 differs.)  |quotient| is at most 127 (1 + 2^-23), so
+// no bound is needed there.
 template <int VEC>
 __device__ __forceinline__ void quants(const float (&y)[VEC], const RowScale &s, unsigned (&q)[VEC])
 {
@@ -674,8 +674,9 @@ cudaError_t launch_shifted(K kernel, const A &a, const ShiftPlan &p, int64_t gri
 
 // Groups per thread: one while the rows alone do not fill the GPU (a call of
 // a few tokens is all latency), four otherwise: two or eight were 10 to 60 %
-// slower on 65536 x 1024 to 8192 x 8192.  Rows off the 16-byte boundaries are
-// taken element by element.
+// slower on 65536 x 1024 to 8192 x 8192.  Rows off the 16-byte boundaries go
+// through shared memory with their shifts (k_rmsnorm_shifted); those of more than
+// 8192 columns, or too wide for it, are taken element by element from memory.
 //   The ring where it pays, us, ring / one row at a time:
 //   x alone in its type     8192 x 8192 bf16 46 / 49, 16384 x 4096 46 / 46,
 //                           65536 x 1024 47 / 42;

@@ -6,8 +6,9 @@
 // and whose hidden states the norm wrote in 8 bits (ember_rmsnorm_quant).
 //
 // Three kernels, by the number of tokens and the rows' alignment:
-//   k_mm_few   up to 4 tokens, up to 8 of a small table: the table is read
-//              once, the products by dp4a; bound by HBM.
+//   k_mm_few   up to 4 tokens, up to 8 by all but large tables, more by a small
+//              table of short rows in groups of 8 while all groups run at once:
+//              each group reads the table once, the products by dp4a; bound by HBM.
 //   k_mm_tc    more tokens: tcgen05 on pairs of CTAs; bound by HBM up to
 //              about 128 tokens, by the tensor cores beyond.
 //   k_mm_any   tables whose rows do not start on 16 bytes.
@@ -17,8 +18,10 @@
 // tensor memory and multiplies in fp16 with fp32 sums.  Products of two
 // 8-bit integers and sums of them below 2^24 are exact in fp32, so the result
 // is the integer one as long as sum_k |xq wq| < 2^24 (always for K <= 1024,
-// and for hidden states and tables in use far beyond); past that a sum is
-// rounded like any fp32 sum.
+// and for hidden states and tables in use far beyond); past that the tensor
+// cores cut the sum off after each step of 16 products, at most two ulps a step.
+// The other two kernels sum 32-bit integers: beyond 2^24 the bits depend on
+// which kernel a call takes, and so on T.
 #include "ember_rows.cuh"
 #include "ember_tc.cuh"
 

@@ -22,6 +22,10 @@ are 2-D with unit stride along their rows; any row stride is accepted.  Calls
 run on torch's current stream, or on `stream` (a torch stream), whose memory
 their outputs and workspace then come from; a tensor that another stream
 still writes has to be waited for by the caller, as with any torch call.
+
+Autograd does not see these calls: outputs carry no history even where an input
+requires a gradient, and tensors written in place keep their version.  The
+gradients are what rmsnorm_backward and softmax_loss return.
 """
 from array import array
 
