@@ -884,11 +884,16 @@ k_mm4_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUten
             const int kb0 = first_block(tile), kb1 = end_block(tile);
             for (int kb = kb0; kb < kb1; ++kb, mine = !mine) {
                 // a stage of the scales is waited for and given back by all, so that
-                // nobody gives one back twice before the others have once
-                if (kb == kb0 || kb % kSBlocks == 0)
+                // nobody gives one back twice before the others have once; the lanes
+                // give up together, whether or not the block is theirs
+                if (kb == kb0 || kb % kSBlocks == 0) {
                     ok = mbar_spin(smem_addr(&tail->sfull[sstage]), sphase, abort, a.wait_ns);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok)
+                        break;
+                }
                 if (mine) {
-                    ok = ok && mbar_spin(smem_addr(&tail->wfull[stage]), phase, abort, a.wait_ns);
+                    ok = mbar_spin(smem_addr(&tail->wfull[stage]), phase, abort, a.wait_ns);
                     const unsigned char *row = smem + (size_t)stage * kTcWBytes + r * 128;
                     const unsigned char *sblock = srow + sstage * kTcSBytes + kb * kSPer % kTcSBox;
 #pragma unroll
