@@ -1060,9 +1060,9 @@ k_mm4_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUten
             for (int64_t i = n > a.bstages ? n - a.bstages : 0; i < n; ++i) {
                 const uint32_t bar = smem_addr(&tail->bfull[i % a.bstages]);
                 if (i >= n0)
-                    mbar_expect_tx(bar, 2 * b_box);
+                    mbar_expect_tx(bar, 4 * b_box);  // a CTA's half of a block
                 else if (i >= n1)
-                    mbar_complete_tx(bar, 2 * b_box);
+                    mbar_complete_tx(bar, 4 * b_box);
                 mbar_wait_final(bar, (uint32_t)(i / a.bstages & 1));
             }
         }
