@@ -66,6 +66,7 @@ struct Cfg {
 constexpr int kMaxCluster = 16;  // CTAs of a row (a non-portable cluster size past 8)
 constexpr int64_t kMaxV = 1 << 19;
 constexpr float kInf = __builtin_huge_valf();
+constexpr float kMaxFloat = 0x1.fffffep127f;
 constexpr double kLog2e = 1.4426950408889634074;
 constexpr double kMaxTemperature = 0x1p100;
 
@@ -174,7 +175,7 @@ __device__ __forceinline__ Weigher make_weigher(float M, const RowSet &r, int S)
     w.m1 = __fadd_rn(__fadd_rn(p, big), -big);
     w.m2 = (p - w.m1) + lo;
     w.start = kGrid + (float)(62 - S) + p;
-    w.cut = from_above(M, -r.d1, -r.d2);
+    w.cut = fmaxf(from_above(M, -r.d1, -r.d2), -kMaxFloat);  // never -inf, which is masked
     return w;
 }
 

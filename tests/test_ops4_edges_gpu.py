@@ -3,6 +3,7 @@ waits that run out in tiles of one block, extreme numbers, settings per row agai
 
 As in test_ops4_gpu.py the tolerances follow from the arithmetic and are stated at each check.
 """
+import math
 import time
 
 import pytest
@@ -10,7 +11,7 @@ import torch
 
 from paper_2607_01455_gb300 import Ops
 from paper_2607_01455_gb300 import ember as E
-from test_ops4_gpu import BF, F32, gen, randn, random_table
+from test_ops4_gpu import BF, F32, check_sample, gen, rand, randn, random_table
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +64,27 @@ def test_product_that_gave_up_has_awaited_its_copies(ops, T, V, K, xt, ot):
     finally:
         ops.set_wait_limit_ns(0)
     assert torch.equal(ops.matmul_quant4(x, *t, dtype=ot), want) and ops.device_status() == E.EMBER_OK
+
+
+# ---- sampling ----
+
+@pytest.mark.parametrize("kw", [dict(), dict(top_k=5), dict(top_p=0.5), dict(min_p=0.5), dict(top_k=600, top_p=0.9)],
+                         ids=str)
+@pytest.mark.parametrize("T,V", [(3, 7), (20, 1001), (400, 777), (310, 8203), (2, 70001)])
+@pytest.mark.parametrize("temperature", [3e29, 4e29, 2.0 ** 100])
+def test_sample_of_the_lowest_logits(ops, T, V, temperature, kw):
+    """Rows of -FLT_MAX and -inf, hot: what is 40 octaves below the largest is no float any
+    more, and -inf stays masked; nor is anything drawn from beside a row (it starts and ends
+    inside a 16-byte unit)."""
+    g = gen(V)
+    low = torch.finfo(F32).min
+    b = torch.full((T, V + 8), math.inf, device="cuda")
+    z = b[:, 3:V + 3]
+    z.copy_(torch.where(rand(g, T, V) < 0.3, low, -math.inf))
+    z[:, V // 2] = low
+    z[::2, V // 3] = 0.9999 * low  # weights of about 1 all the same, but not quite equal
+    u = rand(g, T)
+    u[0] = 1 - 2.0 ** -24
+    for a in (temperature, torch.full((T,), temperature, device="cuda")):
+        ids, lp = check_sample(ops, z, u, temperature=a, **kw)
+        assert (z.gather(1, ids[:, None]) > -math.inf).all() and torch.isfinite(lp).all()
