@@ -982,7 +982,7 @@ struct Draw {
 
     // top-p.  One atomic addition per logit: of its weight's leading 12 bits (so that a
     // whole row's stay within 32), which give the sums by bin to 2^-10 of themselves,
-    // from below, and so one or two bins for the cut.  A second pass adds up what is before these, exactly, and
+    // from below but for a unit per logit, and so one or two bins for the cut.  A second pass adds up what is before these, exactly, and
     // collects their logits; with the cut among those known, the kept sums of the
     // warps are too, `mine` by thread, and no third pass is needed.  Returns
     // whether that is so: not where the bins have more logits than the list holds, nor
@@ -1033,7 +1033,8 @@ struct Draw {
             const u64 end = sum_at(coarse + lane, 0);
             u64 low, high;
             const int first = search<K::fine_bins>(bins, end, 0, [&](u64 g) { return g + (g >> 10) + kBins >= goal; }, low, high);
-            const int last = search<K::fine_bins>(bins, end, 0, [&](u64 g) { return g >= goal; }, low, high);
+            // (below the unit a weight's leading bits exceed the weight, by less than one unit each)
+            const int last = search<K::fine_bins>(bins, end, 0, [&](u64 g) { return g >= goal + (u64)row.V; }, low, high);
             if (lane == 0) {
                 s->bin = first;
                 s->base = (u64)(last < 0 ? kBins - 1 : last);

@@ -5,6 +5,7 @@ As in test_ops4_gpu.py the tolerances follow from the arithmetic and are stated 
 """
 import math
 import time
+from fractions import Fraction
 
 import pytest
 import torch
@@ -88,3 +89,35 @@ def test_sample_of_the_lowest_logits(ops, T, V, temperature, kw):
     for a in (temperature, torch.full((T,), temperature, device="cuda")):
         ids, lp = check_sample(ops, z, u, temperature=a, **kw)
         assert (z.gather(1, ids[:, None]) > -math.inf).all() and torch.isfinite(lp).all()
+
+
+@pytest.mark.parametrize("n", [200, 1000])
+@pytest.mark.parametrize("T,V", [(310, 8000), (310, 20000), (2, 60000)])
+def test_sample_top_p_cuts_behind_the_smallest_weights(ops, T, V, n):
+    """n weights of 105 units and behind them n of 95, and a top-p that takes a few of the latter:
+    the sum of the leading bits of the former, which go past the unit, has reached it before."""
+    def logit(octave, low, high):
+        """A logit about so far below a largest one of 0, and its weight in units of 2^-46: a whole
+        number, what is cut off between `low` and `high`, that is odd and so stays as it is."""
+        z = torch.tensor(-octave * math.log(2.0))
+        while True:
+            w = math.exp(z.item()) * 2.0 ** 46
+            if int(w) % 2 and low < w - int(w) < high:
+                return z.item(), int(w)
+            z = torch.nextafter(z, torch.tensor(-100.0))
+
+    (za, wa), (zb, wb) = logit(39.25, 0.85, 0.95), logit(39.40, 0.3, 0.7)
+    # at the first's end the sum of the exact integers, and of all
+    upto, mass = 2 ** 46 + n * wa, 2 ** 46 + n * (wa + wb)
+    top_p = (upto + 0.4 * n) / mass  # exact to a unit
+    goal = -(-Fraction(top_p) * mass // 1)
+    assert upto < goal < upto + 0.8 * n and wb < wa
+    kept = -(-(goal - upto) // wb)
+    total = upto + kept * wb
+    z = torch.full((T, V), -math.inf, device="cuda")
+    b0, a0, at = 5, V // 3, V - 2
+    z[:, b0:b0 + n], z[:, a0:a0 + n], z[:, at] = zb, za, 0.0
+    for place, want in ((kept * wb - wb / 2, b0 + kept - 1), (kept * wb + wa / 2, a0),
+                        (kept * wb + n * wa - wa / 2, a0 + n - 1), (kept * wb + n * wa + wa / 2, at)):
+        ids, _ = ops.sample(z, torch.full((T,), float(place / total), device="cuda"), top_p=top_p)
+        assert (ids == want).all(), (ids[:10], want)
