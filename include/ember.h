@@ -508,9 +508,12 @@ ember_status ember_matmul_nibble(const void *x, int64_t ldx, ember_wdtype xtype,
  * counts as 0, u >= 1 as the largest below 1.  -inf masks a logit out.  A row
  * that is -inf throughout, one with a NaN or +inf among its logits, and one
  * whose own temperature is negative, NaN or too large has no distribution: its
- * id is -1 and its log-probability NaN.  The weights are summed exactly in
- * units of 2^-46 (of 2^-44 for V = 524288), each good to about 2^-33 of its
- * value: the same row gives the same token in every call.  V <= 524288. */
+ * id is -1 and its log-probability NaN.  For the filters and the draw the
+ * weights are whole numbers of units of 2^-46 (2^-45 for V past 131072, 2^-44 past
+ * 262144), each good to 2^-33 of its value or to one unit, whichever is more, and
+ * their sums are exact: the same row gives the same token in every call.  A
+ * log-probability is that of the weight itself, to fp32 for the rarest
+ * token too.  V <= 524288. */
 ember_status ember_sample(const void *logits, int64_t ldz, ember_wdtype ztype, const float *u, int64_t T, int64_t V,
                           double temperature, const float *temperatures, int64_t top_k, const int32_t *top_ks,
                           double top_p, const float *top_ps, double min_p, const float *min_ps, int64_t *ids,

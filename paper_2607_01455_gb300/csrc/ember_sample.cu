@@ -17,7 +17,7 @@
 // and then, differently for every order of summation.  So the weights are 64-bit
 // integers, units of 2^-S, whose sums are exact, the same for every grouping:
 // the result depends on nothing but the row.  A weight itself is good to about
-// 2^-33 of its value (see Weigher), with errors of either sign.
+// 2^-33 of its value (see Weigher) or to a unit, with errors of either sign.
 //
 // A row is read once from HBM and a few times from L2; a logit's weight takes some 22
 // instructions a time.  Passes over a row: the largest logit, the kept weights' sums by
@@ -234,6 +234,15 @@ struct Weight {
         u64 a, b;
         pair(z, z, a, b);
         return a;
+    }
+    // (M - z) / a of a logit that counts: ln 2 (k + g), k 256 and ln 2 in two parts.
+    __device__ __forceinline__ float fall(float z) const
+    {
+        constexpr double l = 0.69314718055994530942;
+        constexpr float l1 = (float)l, l2 = (float)(l - (double)l1);
+        const float x = z - k.z0, n = __fmaf_rn(x, -k.c1, k.start) - grid;
+        const float g = __fmaf_rn(x, -k.c1, k.m1 - n) + __fmaf_rn(x, -k.c2, k.m2);
+        return __fmaf_rn(n, l1, __fmaf_rn(g, l1, n * l2));
     }
 };
 
@@ -628,9 +637,14 @@ struct Draw {
         }
         __syncthreads();  // the row and s->part have been read
     }
-    __device__ __forceinline__ float log_share(u64 w, u64 total) const
+    // The log-probability of a logit of weight w among weights of the sum `total`.
+    // The integer of a small weight has few bits (none to spare below 2^24 units, six
+    // or four at the cut): its logarithm is taken from the logit itself.
+    __device__ __forceinline__ float log_share(float z, u64 w, u64 total) const
     {
         const float rest = (float)(total - w), all = (float)total;
+        if (w < 1u << 24)
+            return -weight.fall(z) - logf(all * __uint_as_float((unsigned)(127 - S) << 23));
         return 2 * w > total ? log1pf(-(rest / all)) : logf((float)w / all);
     }
 
@@ -1215,7 +1229,7 @@ struct Draw {
                 sum += __shfl_xor_sync(0xffffffffu, sum, o);
             if (sum <= at && at < sum + e.w && sub == 0 && i < n) {
                 *id = e.v;
-                *logprob = log_share(e.w, total);
+                *logprob = log_share(e.z, e.w, total);
             }
         }
     }
@@ -1244,7 +1258,7 @@ struct Draw {
         const unsigned i = select(list, n, [](const Entry &e) { return (u64)(unsigned)e.v; }, weight_of, 0, at + 1);
         if (tid == 0) {
             *id = list[i].v;
-            *logprob = log_share(list[i].w, total);
+            *logprob = log_share(list[i].z, list[i].w, total);
         }
     }
 };
@@ -1358,9 +1372,9 @@ __global__ void __launch_bounds__(Cfg<FORM>::threads, sample_ctas(FILTER, FORM))
                     d.locate(
                         goal - before, [&](const float(&x)[VE], int v) { return d.unit_sum(keep, x, v); },
                         [&](float x, int v) { return keep(x, v) ? d.weight(x) : (u64)0; },
-                        [&](float, int v, u64 w) {
+                        [&](float x, int v, u64 w) {
                             a.ids[t] = v;
-                            a.logprobs[t] = greedy ? 0.f : d.log_share(w, total);
+                            a.logprobs[t] = greedy ? 0.f : d.log_share(x, w, total);
                         });
             }
         }

@@ -121,3 +121,26 @@ def test_sample_top_p_cuts_behind_the_smallest_weights(ops, T, V, n):
                         (kept * wb + n * wa - wa / 2, a0 + n - 1), (kept * wb + n * wa + wa / 2, at)):
         ids, _ = ops.sample(z, torch.full((T,), float(place / total), device="cuda"), top_p=top_p)
         assert (ids == want).all(), (ids[:10], want)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,V", [(40, 1000), (200, 5000), (40, 20000), (310, 20000), (3, 60000), (3, 524288)])
+@pytest.mark.parametrize("shift,temperature", [(0.0, 1.0), (40.0, 0.7), (-3000.0, 0.05), (0.0, 2.0 ** 90)])
+@pytest.mark.parametrize("others,kw", [(40, dict()), (40, dict(top_k=41)), (300, dict(top_k=301)),
+                                       (300, dict(top_p=1 - 2.0 ** -45))], ids=str)
+def test_sample_log_probabilities_of_the_rarest(ops, T, V, shift, temperature, others, kw, dtype):
+    """u = 0 draws the first token, however small its weight: 18 to 38 octaves below the largest."""
+    g = gen(V)
+    z = torch.full((T, V), -math.inf, device="cuda")
+    z[:, 5:5 + others] = (shift - temperature * randn(g, T, others).abs()).to(dtype).float()
+    z[:, 7] = shift
+    octaves = torch.linspace(18, 35 if "top_p" in kw else 38, T, device="cuda")  # (a top-p that keeps it)
+    z[:, 0] = shift - temperature * math.log(2.0) * octaves
+    z = z.to(dtype)
+    ids, lp = ops.sample(z, torch.zeros(T, device="cuda"), temperature=temperature, **kw)
+    d = (z.double() - z.double().amax(1, keepdim=True)) / temperature
+    want = d[:, 0] - torch.logsumexp(torch.where(d > -40 * math.log(2.0), d, -math.inf), 1)
+    assert (ids == 0).all()
+    # |want| is 12 to 33: its rounding, that of (z - M) / a, two ulps of the sum's logarithm (below 8)
+    # and one of their difference are 2^-24 (33 + 33 + 2 8) + 2^-33 or so, below 6e-6
+    assert ((lp.double() - want).abs() <= 6e-6).all(), (lp.double() - want).abs().max()
