@@ -52,17 +52,28 @@ __device__ __forceinline__ float load_x(const void *x, int xf32, int64_t at)
 
 // Rows at any address: tiles of 64 channels x 16 tokens through shared memory
 // as fp32, loaded byte by byte.  Takes what the kernels with 16-byte loads
-// cannot.
+// cannot.  The power of two in a row's scale is in its values already (they stay
+// exact), so that large states overflow in results alone.
 constexpr int kGV = 64, kGT = 16, kGK = 64;
+__device__ __forceinline__ int scale_exponent(float r)  // of a normal number, below 2^100
+{
+    const int e = (int)(__float_as_uint(r) >> 23 & 255u);
+    return e == 0 || e == 255 ? 0 : e > 227 ? 100 : e - 127;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 __global__ void __launch_bounds__(256) k_mm4_any(Mm4Args a, unsigned vblocks)
 {
     __shared__ float sx[kGT][kGK + 1];
     __shared__ float sw[kGV][kGK + 1];
+    __shared__ float sp[kGV];
     const int64_t v0 = (int64_t)(blockIdx.x % vblocks) * kGV, t0 = (int64_t)(blockIdx.x / vblocks) * kGT;
     const int tv = threadIdx.x & 63, tt = threadIdx.x >> 6;
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
     dev::grid_dep_wait();
     dev::grid_dep_launch();
+    if (threadIdx.x < kGV)
+        sp[threadIdx.x] = v0 + threadIdx.x < a.V ? power_of_two(scale_exponent(a.scales[v0 + threadIdx.x])) : 0.f;
+    __syncthreads();
     for (int k0 = 0; k0 < a.K; k0 += kGK) {
         for (int i = threadIdx.x; i < kGT * kGK; i += 256) {
             const int r = i / kGK, k = i % kGK;
@@ -73,7 +84,7 @@ __global__ void __launch_bounds__(256) k_mm4_any(Mm4Args a, unsigned vblocks)
             float lo = 0.f, hi = 0.f;
             if (k0 + k < a.K && v0 + r < a.V) {
                 const unsigned c = a.codes[(v0 + r) * a.ldc + (k0 + k) / 2];
-                const float s = e4m3_value(a.gscales[(v0 + r) * a.ldg + ((k0 + k) >> a.log_group)]);
+                const float s = sp[r] * e4m3_value(a.gscales[(v0 + r) * a.ldg + ((k0 + k) >> a.log_group)]);
                 lo = (float)((int)(c & 15u) - 8) * s;
                 hi = k0 + k + 1 < a.K ? (float)((int)(c >> 4) - 8) * s : 0.f;
             }
@@ -93,7 +104,7 @@ __global__ void __launch_bounds__(256) k_mm4_any(Mm4Args a, unsigned vblocks)
     const int64_t v = v0 + tv;
     if (v >= a.V)
         return;
-    const float r = a.scales[v];
+    const float r = a.scales[v] * power_of_two(-scale_exponent(a.scales[v]));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t t = t0 + tt + 4 * j;
@@ -444,7 +455,7 @@ k_mm4_few(const __grid_constant__ CUtensorMap tm, const Mm4Args a, const FewPlan
                     sum += tile_join[(k * kBoxRows + r) * kFewCols + q * T + tok];
             const int64_t v = (int64_t)tile * kBoxRows + r;
             if (v < a.V)
-                store_out(a.out, a.obf16, tok * a.ldo + v, sum * back[tok] * a.scales[v]);
+                store_out(a.out, a.obf16, tok * a.ldo + v, sum * a.scales[v] * back[tok]);
         }
         tile_sync();
     }
@@ -583,10 +594,10 @@ __device__ __forceinline__ void write_cols4(T *p, int64_t ldo, float (&d)[32], c
 {
     const f2 r2 = make2(r, r);
 #pragma unroll
-    for (int e = 0; e < 32; e += 4) {  // a power of two first: one rounding
+    for (int e = 0; e < 32; e += 4) {  // the power of two last: one rounding, and large states overflow in results alone
         const float4 b = *reinterpret_cast<const float4 *>(back + e);
-        split2(mul2(mul2(make2(d[e], d[e + 1]), make2(b.x, b.y)), r2), d[e], d[e + 1]);
-        split2(mul2(mul2(make2(d[e + 2], d[e + 3]), make2(b.z, b.w)), r2), d[e + 2], d[e + 3]);
+        split2(mul2(mul2(make2(d[e], d[e + 1]), r2), make2(b.x, b.y)), d[e], d[e + 1]);
+        split2(mul2(mul2(make2(d[e + 2], d[e + 3]), r2), make2(b.z, b.w)), d[e + 2], d[e + 3]);
     }
     if (!on)
         return;
@@ -1089,7 +1100,7 @@ __global__ void __launch_bounds__(256) k_mm4_join(const Tc4Args a)
 #pragma unroll 4
     for (int k = 0; k < a.split; ++k)
         s += a.part[((int64_t)k * a.T + t) * a.V + v];
-    store_out(a.out, a.obf16, t * a.ldo + v, s * a.back[t] * a.scales[v]);
+    store_out(a.out, a.obf16, t * a.ldo + v, s * a.scales[v] * a.back[t]);
 }
 
 // Blocks of tokens, all of one width N (a multiple of 32).  One when they fit;

@@ -12,7 +12,7 @@ import torch
 
 from paper_2607_01455_gb300 import Ops
 from paper_2607_01455_gb300 import ember as E
-from test_ops4_gpu import BF, F32, check_sample, gen, rand, randn, random_table
+from test_ops4_gpu import BF, F32, U, check_product, check_sample, gen, rand, randn, random_table, table64
 
 pytestmark = pytest.mark.gpu
 
@@ -65,6 +65,39 @@ def test_product_that_gave_up_has_awaited_its_copies(ops, T, V, K, xt, ot):
     finally:
         ops.set_wait_limit_ns(0)
     assert torch.equal(ops.matmul_quant4(x, *t, dtype=ot), want) and ops.device_status() == E.EMBER_OK
+
+
+@pytest.mark.parametrize("xt,ot", [(BF, F32), (F32, F32), (BF, BF)])
+@pytest.mark.parametrize("kw", [dict(), dict(pad_c=1)], ids=str)
+@pytest.mark.parametrize("T,V,K", [(1, 333, 500), (8, 333, 500), (40, 333, 500), (130, 700, 500), (40, 256, 8192)])
+def test_product_of_large_states_is_finite_where_its_results_are(ops, T, V, K, kw, xt, ot):
+    """States of 1e35 and more: their products with q s, up to 3136 each, are past the floats before
+    the row's scale of 1e-5 brings them back."""
+    g = gen(K + T)
+    got = check_product(ops, (randn(g, T, K) * 1e36).to(xt), random_table(g, V, K, 32, **kw), 32, ot)
+    assert torch.isfinite(got).all()
+
+
+def check_each_row(ops, x, t):
+    """Against 64 bits, each output by its own row's size: fp32 states of K = 64 with twice 4 steps of
+    16 products, each cut off by two ulps of the sum of magnitudes at most or a plain chain of 64 sums,
+    states off by 2 u, a group's sum, two joins and the row's scale by u each: (128 + 8) u."""
+    got = ops.matmul_quant4(x, *t, dtype=F32)
+    q, r = table64(*t, x.shape[1], 32)
+    want, terms = x.double() @ (q * r).T, x.double().abs() @ (q * r).abs().T
+    assert ((got.double() - want).abs() <= 136 * U * terms).all(), ((got.double() - want).abs() / terms).max()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(pad_c=1)], ids=str)
+@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("size", [2.0 ** -30, 1.0, 2.0 ** 20])
+def test_product_with_rows_of_extreme_scales(ops, T, size, kw):
+    """Row scales from 2^-100 to 2^80, whose results are all within the normal floats."""
+    g = gen(77)
+    V, K = 180, 64
+    codes, gs, _ = random_table(g, V, K, 32, **kw)
+    s = torch.ldexp(1 + rand(g, V), torch.arange(-100, V - 100, device="cuda"))
+    check_each_row(ops, randn(g, T, K) * size, (codes, gs, s))
 
 
 # ---- sampling ----
