@@ -268,10 +268,11 @@ k_mm4_few(const __grid_constant__ CUtensorMap tm, const Mm4Args a, const FewPlan
     if (threadIdx.x < kFewCols)
         tops[threadIdx.x] = 0;
     __syncthreads();
-    // the copies: box `pb` of tile `pt` is the next one; they do not wait for the
-    // kernels before this one unless those may have written the table
+    // the copies: box `pb` of tile `pt` is the next one
     dev::grid_dep_wait();
     dev::grid_dep_launch();
+    if (lane == 0)  // the kernel before this one may have written the table, by plain stores
+        asm volatile("fence.proxy.async.global;" ::: "memory");
     unsigned char *const ring = smem + p.ring_at + (size_t)warp * p.stages * kBoxBytes;
     const uint32_t ring_addr = tc::smem_addr(ring);
     int pt = tile0, pb = b0, pstage = 0;
@@ -718,6 +719,7 @@ k_mm4_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUten
         int stage = 0;
         uint32_t phase = 0;
         int64_t issued = 0;
+        asm volatile("fence.proxy.async.global;" ::: "memory");  // as below
         const uint64_t pol = l2_policy(a.ntb > 1 ? 0 : 2);
         bool ok = true;
         for (int tile = tile0; tile < ntiles && ok; tile += tstep) {
@@ -749,7 +751,8 @@ k_mm4_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUten
         int stage = 0;
         uint32_t phase = 0;
         int64_t issued = 0;  // blocks whose copies were issued
-        asm volatile("fence.proxy.async.global;" ::: "memory");  // the tokens were written by plain stores
+        // the tokens were written by plain stores, and the table may have been
+        asm volatile("fence.proxy.async.global;" ::: "memory");
         // the table streams when every block is read once
         const uint64_t pol = l2_policy(tokens ? 1 : a.ntb > 1 ? 0 : 2);
         bool ok = true;
