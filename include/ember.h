@@ -471,15 +471,19 @@ ember_status ember_dequantize_rows_nibble(const uint8_t *codes, int64_t ldc, con
 
 /* Product with such a table: out[t][v] = r_v sum_k x[t][k] q_vk s_v,k/group.
  *   x: T x K of xtype; the table has V rows of K values; out: T x V of otype.
- * Hidden states become fp16 numbers over a power of two per token, one for bf16,
- * the sum of two for fp32: exact, or off by 2^-24 of a number (fp32), where it is
- * above 2^-28 of the token's largest magnitude, and off by 2^-39 of that
- * magnitude below.  The products are exact; the sums are fp32, on the tensor cores
+ * Hidden states become fp16 numbers over a power of two per token, one for bf16
+ * (exact where it is above 2^-31 of the token's largest magnitude, off by 2^-39 of that
+ * magnitude at most below), the sum of two for fp32 (off by 2^-23 of the number or by
+ * 2^-39 of that magnitude, whichever is more: 2^-23 of numbers above 2^-16 of it);
+ * or off by 2^-152, for tokens whose largest magnitude is below 2^-113.
+ * The products are exact; the sums are fp32, on the tensor cores
  * cut off (not rounded) after each step of 16 products, so a row's last bits may
  * depend on T.  Outputs in fp32 are sums of blocks of at most 256 products, rounded
  * at each block.  An infinity or a NaN among a token's states makes its row infinite or NaN,
  * one among a row's scales its column.  Only tables whose codes and scales start
- * on 16 bytes row by row take the tensor cores.  K <= 32768.  T = 0 does nothing.  workspace:
+ * on 16 bytes row by row take the tensor cores; others (a copy that dropped the padding
+ * between rows) are read byte by byte, their states as they are, 10 to 100 times
+ * slower.  K <= 32768.  T = 0 does nothing.  workspace:
  * ember_matmul_nibble_workspace_bytes(T, V, K, xtype).  status (not NULL):
  * EMBER_ERR_TIMEOUT if a bounded wait gave up. */
 size_t ember_matmul_nibble_workspace_bytes(int64_t T, int64_t V, int64_t K, ember_wdtype xtype);

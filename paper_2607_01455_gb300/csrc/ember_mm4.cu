@@ -114,9 +114,10 @@ __global__ void __launch_bounds__(256) k_mm4_any(Mm4Args a, unsigned vblocks)
 }
 
 // Hidden states as fp16, scaled by a power of two per token (token_scale) that
-// brings the largest below 2^15.  A bf16 number is exact then, or below 2^-28 of
-// the token's largest and off by 2^-39 of it at most; an fp32 number becomes a sum
-// of two, p[0] + p[1], off by 2^-24 of itself.  Eight from k on (zeros behind K),
+// brings the largest into [2^14, 2^15).  A bf16 number is exact then, or below 2^-31 of
+// the token's largest and off by 2^-39 of it at most, half of fp16's last step; an fp32
+// number becomes a sum of two of 11 bits, p[0] + p[1], off by 2^-23 of itself or by
+// as much as a bf16 number, which is more below 2^-16 of the largest.  Eight from k on (zeros behind K),
 // in the order 0 4 1 5 2 6 3 7, that of the codes.
 template <typename XT> constexpr int kParts = sizeof(XT) == 4 ? 2 : 1;
 template <typename XT>

@@ -100,6 +100,31 @@ def test_product_with_rows_of_extreme_scales(ops, T, size, kw):
     check_each_row(ops, randn(g, T, K) * size, (codes, gs, s))
 
 
+@pytest.mark.parametrize("xt", [BF, F32])
+@pytest.mark.parametrize("T,V,K", [(1, 200, 96), (4, 200, 2100), (40, 200, 96), (40, 200, 4096), (130, 300, 300)])
+def test_states_beside_a_huge_channel(ops, T, V, K, xt):
+    """A channel that no row of the table uses sets the token's power of two: other states are off by
+    2^-23 of themselves (bf16: by nothing) or by 2^-39 of it."""
+    g = gen(K)
+    huge, at = K // 3, K // 2 + 1
+    codes, gs, s = random_table(g, V, K, 32)
+    byte = codes[:, huge // 2]
+    codes[:, huge // 2] = (byte & 0xF0) | 8 if huge % 2 == 0 else (byte & 0x0F) | 0x80
+    x = torch.zeros(T, K, device="cuda")
+    x[:, huge] = (1 + rand(g, T)) * 1000
+    x[:, at] = x[:, huge] * (0.5 + rand(g, T)) * torch.exp2(torch.linspace(-1, -38, T, device="cuda"))
+    x = x.to(xt)
+    got = ops.matmul_quant4(x, codes, gs, s, dtype=F32)
+    q, r = table64(codes, gs, s, K, 32)
+    x, w = x.double(), (q * r)[:, at]
+    off = torch.maximum((0.0 if xt == BF else 2.0 ** -23) * x[:, at].abs(), 2.0 ** -39 * x[:, huge])
+    if xt == BF:
+        off[x[:, at] > 2.0 ** -31 * x[:, huge]] = 0
+    # and one step that sums the two parts, cut off by two ulps at most, and the row's scale
+    bound = off[:, None] * w.abs() + 5 * U * x[:, at, None] * w.abs()
+    assert ((got.double() - x[:, at, None] * w).abs() <= bound).all()
+
+
 # ---- sampling ----
 
 @pytest.mark.parametrize("kw", [dict(), dict(top_k=5), dict(top_p=0.5), dict(min_p=0.5), dict(top_k=600, top_p=0.9)],
