@@ -125,6 +125,39 @@ def test_states_beside_a_huge_channel(ops, T, V, K, xt):
     assert ((got.double() - x[:, at, None] * w).abs() <= bound).all()
 
 
+@pytest.mark.parametrize("T,V", [(1, 300), (4, 300), (9, 300), (40, 300), (40, 20000), (130, 3000)])
+@pytest.mark.parametrize("K", [2049, 4096])
+def test_fp32_states_are_not_rounded_in_any_block(ops, T, V, K):
+    """One product per sum, in the first block of K, in others and in the last: the state is off by 2 u,
+    the step that sums its parts by two ulps, the row's scale by u: 7 u.  (fp16 states are off by 2^12 u.)"""
+    g = gen(T)
+    t = random_table(g, V, K, 32)
+    q, r = table64(*t, K, 32)
+    for at in (0, 255, 256, 1000, K // 2 + 3, K - 1):
+        x = torch.zeros(T, K, device="cuda")
+        x[:, at] = randn(g, T) * torch.exp(20 * randn(g, T))
+        got = ops.matmul_quant4(x, *t, dtype=F32)
+        want = x[:, at].double()[:, None] * (q * r)[:, at]
+        assert ((got.double() - want).abs() <= 7 * U * want.abs()).all()
+
+
+@pytest.mark.parametrize("T,V", [(4, 3000), (40, 1000), (40, 20000), (300, 2000)])
+@pytest.mark.parametrize("K", [1000, 2049, 4096, 8192])
+def test_fp32_sums_do_not_lose_more_with_their_length(ops, T, V, K):
+    """In root mean square, as a share of |x| |w|.  A step of 16 products cuts the sum so far off by half of
+    its last place on average, 0.7 2^-24 of it, and a block's sum grows with the root of its steps: 16 steps
+    of a block of 256 (the small parts' are nothing beside them) lose 16 0.7 2^-24 2/3 of the block's |x| |w|
+    and its sign, blocks one another's at random: 2^-21.1.  The blocks' own 32 roundings leave 2^-24 or so.  Four
+    times that is the limit; fp16 states leave 2^-13, one sum over all of K = 2049 2^-18.1, of 8192 2^-16."""
+    g = gen(K + T)
+    x, t = randn(g, T, K), random_table(g, V, K, 64)
+    q, r = table64(*t, K, 64)
+    w = q * r
+    err = ops.matmul_quant4(x, *t, group=64, dtype=F32).double() - x.double() @ w.T
+    size = x.double().norm(dim=1)[:, None] * w.norm(dim=1)
+    assert (err / size).square().mean().sqrt() <= 2.0 ** -19.1
+
+
 # ---- sampling ----
 
 @pytest.mark.parametrize("kw", [dict(), dict(top_k=5), dict(top_p=0.5), dict(min_p=0.5), dict(top_k=600, top_p=0.9)],
