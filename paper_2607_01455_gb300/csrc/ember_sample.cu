@@ -460,15 +460,6 @@ struct Draw {
             fn(z, row.v0 + q * VE);
         }
     }
-    template <typename F>
-    __device__ __forceinline__ void each(F fn) const
-    {
-        each_unit([&](const float(&z)[VE], int v) {
-#pragma unroll
-            for (int e = 0; e < VE; ++e)
-                fn(z[e], v + e);
-        });
-    }
     __device__ __forceinline__ float largest() const
     {
         const int m = share(), end = (warp + 1) * m < row.n ? (warp + 1) * m : row.n;

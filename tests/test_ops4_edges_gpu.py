@@ -12,7 +12,7 @@ import torch
 
 from paper_2607_01455_gb300 import Ops
 from paper_2607_01455_gb300 import ember as E
-from test_ops4_gpu import BF, F32, U, check_product, check_sample, gen, rand, randn, random_table, table64
+from test_ops4_gpu import BF, F32, U, check_product, check_sample, gen, logits_of, rand, randn, random_table, table64
 
 pytestmark = pytest.mark.gpu
 
@@ -235,3 +235,24 @@ def test_sample_log_probabilities_of_the_rarest(ops, T, V, shift, temperature, o
     # |want| is 12 to 33: its rounding, that of (z - M) / a, two ulps of the sum's logarithm (below 8)
     # and one of their difference are 2^-24 (33 + 33 + 2 8) + 2^-33 or so, below 6e-6
     assert ((lp.double() - want).abs() <= 6e-6).all(), (lp.double() - want).abs().max()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,V", [(64, 1000), (24, 50257), (160, 4000), (310, 20000)])
+def test_sample_settings_per_row_are_those_of_a_call(ops, T, V, dtype):
+    """A row of a batch with settings of its own against that row alone with the same numbers, whose
+    constants the host makes: the same token and the same bits of its log-probability."""
+    g = gen(V)
+    z, u = logits_of(g, T, V, dtype), rand(g, T)
+    z[:, V - V // 50:] = -math.inf
+    a = torch.exp(randn(g, T))
+    a[::9] = 0
+    k = torch.where(rand(g, T) < 0.5, 0, (1 + 300 * rand(g, T)).int()).int()
+    p = torch.where(rand(g, T) < 0.3, 1.0, 0.5 + 0.5 * rand(g, T))
+    m = torch.where(rand(g, T) < 0.5, 0.0, 0.2 * rand(g, T))
+    m[1::16], p[2::16] = 1.0, 1e-3
+    ids, lp = ops.sample(z, u, temperature=a, top_k=k, top_p=p, min_p=m)
+    for t in range(T):
+        i1, l1 = ops.sample(z[t:t + 1], u[t:t + 1], temperature=a[t].item(), top_k=k[t].item(), top_p=p[t].item(),
+                            min_p=m[t].item())
+        assert i1[0] == ids[t] and l1[0] == lp[t], t
