@@ -26,6 +26,7 @@ using namespace rows;
 using namespace quant4;
 
 constexpr int64_t kMaxMmRows = INT32_MAX - 1024;  // row numbers of a last tile stay within 32 bits
+constexpr float kMaxFloat = 0x1.fffffep127f;
 
 struct Mm4Args {
     const void *x;
@@ -52,15 +53,17 @@ __device__ __forceinline__ float load_x(const void *x, int xf32, int64_t at)
 
 // Rows at any address: tiles of 64 channels x 16 tokens through shared memory
 // as fp32, loaded byte by byte.  Takes what the kernels with 16-byte loads
-// cannot.  The power of two in a row's scale is in its values already (they stay
-// exact), so that large states overflow in results alone.
+// cannot.  Sums that pass the floats are formed again with the power of two in the
+// rows' scales in the values already (which stay exact), so that large states
+// overflow in results alone (in every sum it costs 3 %: 1471 -> 1510 us on 1 x 128256 x 4096).
 constexpr int kGV = 64, kGT = 16, kGK = 64;
-__device__ __forceinline__ int scale_exponent(float r)  // of a normal number, below 2^100
+__device__ __forceinline__ int scale_exponent(float r)  // of a normal number, at most 100
 {
     const int e = (int)(__float_as_uint(r) >> 23 & 255u);
     return e == 0 || e == 255 ? 0 : e > 227 ? 100 : e - 127;
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
+
 __global__ void __launch_bounds__(256) k_mm4_any(Mm4Args a, unsigned vblocks)
 {
     __shared__ float sx[kGT][kGK + 1];
@@ -71,40 +74,57 @@ __global__ void __launch_bounds__(256) k_mm4_any(Mm4Args a, unsigned vblocks)
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
     dev::grid_dep_wait();
     dev::grid_dep_launch();
-    if (threadIdx.x < kGV)
-        sp[threadIdx.x] = v0 + threadIdx.x < a.V ? power_of_two(scale_exponent(a.scales[v0 + threadIdx.x])) : 0.f;
-    __syncthreads();
-    for (int k0 = 0; k0 < a.K; k0 += kGK) {
-        for (int i = threadIdx.x; i < kGT * kGK; i += 256) {
-            const int r = i / kGK, k = i % kGK;
-            sx[r][k] = k0 + k < a.K && t0 + r < a.T ? load_x(a.x, a.xf32, (t0 + r) * a.ldx + k0 + k) : 0.f;
-        }
-        for (int i = threadIdx.x; i < kGV * kGK / 2; i += 256) {
-            const int r = i / (kGK / 2), k = i % (kGK / 2) * 2;
-            float lo = 0.f, hi = 0.f;
-            if (k0 + k < a.K && v0 + r < a.V) {
-                const unsigned c = a.codes[(v0 + r) * a.ldc + (k0 + k) / 2];
-                const float s = sp[r] * e4m3_value(a.gscales[(v0 + r) * a.ldg + ((k0 + k) >> a.log_group)]);
-                lo = (float)((int)(c & 15u) - 8) * s;
-                hi = k0 + k + 1 < a.K ? (float)((int)(c >> 4) - 8) * s : 0.f;
+    auto sums = [&](auto scaled) {
+        for (int k0 = 0; k0 < a.K; k0 += kGK) {
+            for (int i = threadIdx.x; i < kGT * kGK; i += 256) {
+                const int r = i / kGK, k = i % kGK;
+                sx[r][k] = k0 + k < a.K && t0 + r < a.T ? load_x(a.x, a.xf32, (t0 + r) * a.ldx + k0 + k) : 0.f;
             }
-            sw[r][k] = lo;
-            sw[r][k + 1] = hi;
-        }
-        __syncthreads();
+            for (int i = threadIdx.x; i < kGV * kGK / 2; i += 256) {
+                const int r = i / (kGK / 2), k = i % (kGK / 2) * 2;
+                float lo = 0.f, hi = 0.f;
+                if (k0 + k < a.K && v0 + r < a.V) {
+                    const unsigned c = a.codes[(v0 + r) * a.ldc + (k0 + k) / 2];
+                    float s = e4m3_value(a.gscales[(v0 + r) * a.ldg + ((k0 + k) >> a.log_group)]);
+                    if constexpr (decltype(scaled)::value)
+                        s *= sp[r];
+                    lo = (float)((int)(c & 15u) - 8) * s;
+                    hi = k0 + k + 1 < a.K ? (float)((int)(c >> 4) - 8) * s : 0.f;
+                }
+                sw[r][k] = lo;
+                sw[r][k + 1] = hi;
+            }
+            __syncthreads();
 #pragma unroll 8
-        for (int k = 0; k < kGK; ++k) {
-            const float w = sw[tv][k];
+            for (int k = 0; k < kGK; ++k) {
+                const float w = sw[tv][k];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                acc[j] = __fmaf_rn(sx[tt + 4 * j][k], w, acc[j]);
+                for (int j = 0; j < 4; ++j)
+                    acc[j] = __fmaf_rn(sx[tt + 4 * j][k], w, acc[j]);
+            }
+            __syncthreads();
         }
-        __syncthreads();
-    }
+    };
+    sums(std::false_type{});
     const int64_t v = v0 + tv;
+    float r = v < a.V ? a.scales[v] : 0.f;
+    bool past = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        past |= !(fabsf(acc[j]) <= kMaxFloat);
+    if (__syncthreads_or(past)) {  // or there are infinities or NaN among the inputs
+        const int e = scale_exponent(r);
+        if (tt == 0)
+            sp[tv] = power_of_two(e);
+        r *= power_of_two(-e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            acc[j] = 0.f;
+        __syncthreads();
+        sums(std::true_type{});
+    }
     if (v >= a.V)
         return;
-    const float r = a.scales[v] * power_of_two(-scale_exponent(a.scales[v]));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t t = t0 + tt + 4 * j;
