@@ -919,16 +919,11 @@ k_mm4_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUten
             const int kb0 = first_block(tile), kb1 = end_block(tile);
             for (int kb = kb0; kb < kb1; ++kb, mine = !mine) {
                 // a stage of the scales is waited for and given back by all, so that
-                // nobody gives one back twice before the others have once; the lanes
-                // give up together, whether or not the block is theirs
-                if (kb == kb0 || kb % kSBlocks == 0) {
+                // nobody gives one back twice before the others have once
+                if (kb == kb0 || kb % kSBlocks == 0)
                     ok = mbar_spin(smem_addr(&tail->sfull[sstage]), sphase, abort, a.wait_ns);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok)
-                        break;
-                }
                 if (mine) {
-                    ok = mbar_spin(smem_addr(&tail->wfull[stage]), phase, abort, a.wait_ns);
+                    ok = ok && mbar_spin(smem_addr(&tail->wfull[stage]), phase, abort, a.wait_ns);
                     const unsigned char *row = smem + (size_t)stage * kTcWBytes + r * 128;
                     const unsigned char *sblock = srow + sstage * kTcSBytes + kb * kSPer % kTcSBox;
 #pragma unroll
@@ -993,6 +988,9 @@ k_mm4_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUten
                     aphase ^= 1u;
                 }
             }
+            // a wait for the scales of a block of the other warps' is voted on with the
+            // next block, or here: the lanes give up together
+            ok = __all_sync(0xffffffffu, ok);
         }
         if (!ok && lane == 0 && !*abort)
             set_timeout(abort, a.flags);
