@@ -235,14 +235,12 @@ struct Weight {
         pair(z, z, a, b);
         return a;
     }
-    // (M - z) / a of a logit that counts: ln 2 (k + g), k 256 and ln 2 in two parts.
-    __device__ __forceinline__ float fall(float z) const
+    // The weight in fp32, in the same units, of a logit that counts: 2^(S - k) 2^-g.
+    __device__ __forceinline__ float value(float z, int S) const
     {
-        constexpr double l = 0.69314718055994530942;
-        constexpr float l1 = (float)l, l2 = (float)(l - (double)l1);
         const float x = z - k.z0, n = __fmaf_rn(x, -k.c1, k.start) - grid;
         const float g = __fmaf_rn(x, -k.c1, k.m1 - n) + __fmaf_rn(x, -k.c2, k.m2);
-        return __fmaf_rn(n, l1, __fmaf_rn(g, l1, n * l2));
+        return exp2f((float)S - n - g);
     }
 };
 
@@ -630,13 +628,12 @@ struct Draw {
     }
     // The log-probability of a logit of weight w among weights of the sum `total`.
     // The integer of a small weight has few bits (none to spare below 2^24 units, six
-    // or four at the cut): its logarithm is taken from the logit itself.
+    // or four at the cut): there it is formed anew, good to 2^-20.
     __device__ __forceinline__ float log_share(float z, u64 w, u64 total) const
     {
         const float rest = (float)(total - w), all = (float)total;
-        if (w < 1u << 24)
-            return -weight.fall(z) - logf(all * __uint_as_float((unsigned)(127 - S) << 23));
-        return 2 * w > total ? log1pf(-(rest / all)) : logf((float)w / all);
+        const float part = w < 1u << 24 ? weight.value(z, S) : (float)w;
+        return 2 * w > total ? log1pf(-(rest / all)) : logf(part / all);
     }
 
     // The sum of a number over the CTAs.

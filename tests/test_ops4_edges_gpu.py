@@ -232,8 +232,8 @@ def test_sample_log_probabilities_of_the_rarest(ops, T, V, shift, temperature, o
     d = (z.double() - z.double().amax(1, keepdim=True)) / temperature
     want = d[:, 0] - torch.logsumexp(torch.where(d > -40 * math.log(2.0), d, -math.inf), 1)
     assert (ids == 0).all()
-    # |want| is 12 to 33: its rounding, that of (z - M) / a, two ulps of the sum's logarithm (below 8)
-    # and one of their difference are 2^-24 (33 + 33 + 2 8) + 2^-33 or so, below 6e-6
+    # |want| is 12 to 36: two ulps of the logarithm, 2^-23 36; of its argument, the exponent's rounding
+    # (of at most 28: 2^-20 ln 2), two ulps of the power and one of the quotient: below 6e-6
     assert ((lp.double() - want).abs() <= 6e-6).all(), (lp.double() - want).abs().max()
 
 
