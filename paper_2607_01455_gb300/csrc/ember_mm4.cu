@@ -920,8 +920,13 @@ k_mm4_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUten
             for (int kb = kb0; kb < kb1; ++kb, mine = !mine) {
                 // a stage of the scales is waited for and given back by all, so that
                 // nobody gives one back twice before the others have once
-                if (kb == kb0 || kb % kSBlocks == 0)
+                if (kb == kb0 || kb % kSBlocks == 0) {
                     ok = mbar_spin(smem_addr(&tail->sfull[sstage]), sphase, abort, a.wait_ns);
+                    // the lanes give up together: here, or with the vote on a block of their own
+                    // (as a vote: 64 x 128256 x 4096 80.4 us, as a sum 79.5)
+                    if (!mine)
+                        ok = !__reduce_or_sync(0xffffffffu, !ok);
+                }
                 if (mine) {
                     ok = ok && mbar_spin(smem_addr(&tail->wfull[stage]), phase, abort, a.wait_ns);
                     const unsigned char *row = smem + (size_t)stage * kTcWBytes + r * 128;
@@ -988,9 +993,6 @@ k_mm4_tc(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUten
                     aphase ^= 1u;
                 }
             }
-            // a wait for the scales of a block of the other warps' is voted on with the
-            // next block, or here: the lanes give up together
-            ok = __all_sync(0xffffffffu, ok);
         }
         if (!ok && lane == 0 && !*abort)
             set_timeout(abort, a.flags);
