@@ -375,7 +375,7 @@ ember_status ember_status_read(unsigned *status, void *stream);
  * of ember_matmul_quant, ember_matmul_nibble and ember_softmax_loss, for the calls of this process
  * from now on; 0 restores the default of 2 s.  A wait that runs past it sets
  * EMBER_ERR_TIMEOUT in the status block, and the kernel returns early with
- * its outputs incomplete.  Host only. */
+ * its outputs incomplete; below 1 us any wait may count as one that did.  Host only. */
 ember_status ember_set_ops_wait_limit(uint64_t ns);
 
 /* Residual addition and root-mean-square norm of T rows of D values:

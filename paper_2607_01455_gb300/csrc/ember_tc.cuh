@@ -113,13 +113,12 @@ __device__ __forceinline__ bool mbar_spin_alone(uint32_t bar, uint32_t parity, u
     if (mbar_look(bar, parity))
         return true;
     const uint64_t t0 = dev::now_ns();
-    for (unsigned tries = 1; limit_ns >= 1000; ++tries) {  // a try may last longer than a limit below that
+    for (unsigned tries = 1;; ++tries) {
         if (mbar_test(bar, parity))
             return true;
         if (tries % 32 == 0 && dev::now_ns() - t0 > limit_ns)
             return false;
     }
-    return false;
 }
 
 // Same, for teardown: no abort check, only the fixed limit kTeardownWaitNs (the

@@ -67,6 +67,24 @@ def test_product_that_gave_up_has_awaited_its_copies(ops, T, V, K, xt, ot):
     assert torch.equal(ops.matmul_quant4(x, *t, dtype=ot), want) and ops.device_status() == E.EMBER_OK
 
 
+@pytest.mark.parametrize("xt", [BF, F32])
+@pytest.mark.parametrize("T,V,K,group", [(1, 65536, 8192, 32), (1, 65536, 4096, 128), (3, 33, 300, 64), (1, 1, 1, 32)])
+def test_product_of_few_tokens_gives_up_at_the_shortest_limit(ops, T, V, K, group, xt):
+    """Every time: also where the copies come in before they are waited for."""
+    g = gen(T)
+    x, t = randn(g, T, K).to(xt), random_table(g, V, K, group)
+    want = ops.matmul_quant4(x, *t, group=group)
+    try:
+        for _ in range(100):
+            ops.set_wait_limit_ns(1)
+            ops.matmul_quant4(x, *t, group=group)
+            assert ops.device_status() == E.EMBER_ERR_TIMEOUT
+            ops.set_wait_limit_ns(0)
+            assert torch.equal(ops.matmul_quant4(x, *t, group=group), want) and ops.device_status() == E.EMBER_OK
+    finally:
+        ops.set_wait_limit_ns(0)
+
+
 @pytest.mark.parametrize("xt,ot", [(BF, F32), (F32, F32), (BF, BF)])
 @pytest.mark.parametrize("kw", [dict(), dict(pad_c=1)], ids=str)
 @pytest.mark.parametrize("T,V,K", [(1, 333, 500), (8, 333, 500), (40, 333, 500), (130, 700, 500), (40, 256, 8192)])
