@@ -482,7 +482,7 @@ ember_status ember_dequantize_rows_nibble(const uint8_t *codes, int64_t ldc, con
  * at each block.  An infinity or a NaN among a token's states makes its row infinite or NaN,
  * one among a row's scales its column.  Only tables whose codes and scales start
  * on 16 bytes row by row take the tensor cores; others (a copy that dropped the padding
- * between rows) are read byte by byte, their states as they are, 10 to 100 times
+ * between rows) are read byte by byte, their states as they are, 10 to 50 times
  * slower.  K <= 32768.  T = 0 does nothing.  workspace:
  * ember_matmul_nibble_workspace_bytes(T, V, K, xtype).  status (not NULL):
  * EMBER_ERR_TIMEOUT if a bounded wait gave up. */

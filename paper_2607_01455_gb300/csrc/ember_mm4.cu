@@ -238,8 +238,8 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], unsigned a0, unsigned a1,
 // lane 4 g + t feeds eight values of rows g, g + 8, ... as they are in one word.
 // 2^log_ks warps of a CTA share a tile's K and join their sums through shared memory.
 // Bound by the instructions that unpack and scale as much as by HBM: 1 x 128256 x 8192
-// in groups of 32 107 to 111 us (5.0 to 5.2 TB/s), of 128 90 us (6.0); 8 tokens, whose
-// columns' loads from shared memory add up, 150 us.
+// in groups of 32 100 to 105 us (5.3 to 5.6 TB/s), of 128 88 us (6.1); 8 tokens, whose
+// columns' loads from shared memory add up, 139 us.
 // A warp whose wait gives up copies and computes nothing more but keeps to the
 // barriers, and sets the timeout flag at its end (in the loop the code for it cost
 // 5 % and more: 1 x 128256 x 8192 105.6 us with it, 100.2 without).
@@ -516,10 +516,11 @@ k_mm4_few(const __grid_constant__ CUtensorMap tm, const Mm4Args a, const FewPlan
 //   warps 8-23   widen: eight warps the even blocks, eight the odd ones, four of
 //                them each half; most of a warp's time for a block are waits and
 //                barriers (1100 clocks of 1770 with all sixteen at every block)
-// Measured: 64 x 128256 x 4096 81 us (820 TFLOP/s, 3.6 TB/s; tensor pipes busy 38 %
-// of the time, the widening warps' chain of wait, unpack, store and barrier the rest), 256 x
-// 32000 x 4096 63 us (1070), 2048 x 32000 x 4096 327 us (1640; 0.85 of the measured
-// peak); fp32 states and outputs 600 x 32000 x 4096 200 us (1570 with both parts).
+// Measured: 64 x 128256 x 4096 81 us (830 TFLOP/s, 3.6 TB/s; tensor pipes busy 38 %
+// of the time, HBM 44 %, ALU 60 %: the widening warps' chain of wait, unpack, store and an
+// arrival at both CTAs bounds it), 256 x 32000 x 4096 62 us (1090), 2048 x 32000 x 4096 327 to
+// 360 us by the power limit (1490 to 1640; 0.77 to 0.85 of the measured peak); fp32 states
+// and outputs 600 x 32000 x 4096 198 us (1590 with both parts).
 // Every wait is bounded; one that gives up sets the timeout flag, stops every
 // role, and the kernel returns after its copies and MMAs in flight are done.
 // The two CTAs may then have issued different numbers of copies of the tokens,
@@ -1278,9 +1279,9 @@ FewPlan few_plan(const Mm4Args &a)
     if (!ring(most))
         return p;
     // The rounds that the SMs need for the tiles, each its boxes' time and about one
-    // box's for the joining: us for 2^0 .. 2^4 warps a tile, 128256 x 8192: - / 115 /
-    // 109 / 124 / 140; 32000 x 4096: 33 / 22 / 24 / 27 / 27; 10000 x 1000: 11 / 7.7 / 6.5
-    // / - / -.  Then no more tiles to a CTA than these rounds need.
+    // box's for the joining: us for 2^0 .. 2^4 warps a tile, 128256 x 8192: 107 / 108 /
+    // 101 / 112 / 121; 32000 x 4096: 21.3 / 18.4 / 20.3 / 22.3 / 23.1; 10000 x 1000: 6.1 / 4.9 /
+    // 4.5 / - / -.  Then no more tiles to a CTA than these rounds need.
     const int64_t tiles = (a.V + kBoxRows - 1) / kBoxRows;
     int64_t best = INT64_MAX;
     for (int l = 0; (1 << l) <= most && (1 << l) <= kboxes; ++l) {
@@ -1315,8 +1316,8 @@ cudaError_t launch_few4(const Mm4Args &a, const FewPlan &p, unsigned *flags, cud
 cudaError_t launch_mm4(const Mm4Args &a, void *workspace, unsigned *flags, cudaStream_t stream)
 {
     if (aligned(a.codes, 16) && a.ldc % 16 == 0 && aligned(a.gscales, 16) && a.ldg % 16 == 0) {
-        // us of the warps' kernel / of tcgen05, bf16: 2 x 128256 x 8192 112 / 150, 5 tokens 139 /
-        // 150, 8 148 / 151; 8 x 32000 x 4096 26 / 29, 8 x 50257 x 768 11.6 / 13.6
+        // us of the warps' kernel / of tcgen05, bf16: 2 x 128256 x 8192 102 / 146, 5 tokens 130 /
+        // 147, 8 139 / 148; 8 x 32000 x 4096 24.4 / 27.3, 8 x 50257 x 768 10.2 / 12.1
         if (a.T * (a.xf32 ? 2 : 1) <= kFewCols) {
             const FewPlan p = few_plan(a);
             auto go = [&](auto lg) {

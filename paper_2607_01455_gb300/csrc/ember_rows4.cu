@@ -111,7 +111,8 @@ __device__ __forceinline__ Raw<XT, 8> load_off(const XT *p, int n, const XT *beg
 // being unit k TPR + i of the row.  What is done once per unit (the group's
 // maximum by shuffles, its scale, addresses) is about as much as what is done
 // for its values: 128256 x 8192 bf16 in units of 8 611 us, of 16 475 (5.6 TB/s; 82 %
-// of the instruction slots taken).  Rows off 16 bytes: 60000 x 2049 153 us (2.0 TB/s).
+// of the instruction slots taken), fp32 688 (6.9).  Rows off 16 bytes: 60000 x 2049 bf16
+// 153 us (2.0 TB/s), fp32 215 (2.6).
 template <typename XT, int TPR, int NU, bool GROUPED>
 __global__ void __launch_bounds__(256) k_quantize4(Rows4Args a)
 {
@@ -291,7 +292,8 @@ struct Back4Args {
 
 constexpr int back_unit(size_t size) { return size == 4 ? 16 : 8; }
 
-// Rows in the table's order or those of given ids, one rounding each.  GROUPED:
+// Rows in the table's order or those of given ids: q s exact, its product with r
+// rounded to fp32 (not at all where r is a power of two), then to bf16.  GROUPED:
 // rows of the output start on 16 bytes (32 of fp32); a thread takes 16 or 8
 // values per step.  Otherwise it takes eight at the output's 16-byte boundaries, whose codes
 // begin inside a word and may lie in two groups; the row's first and last few go
